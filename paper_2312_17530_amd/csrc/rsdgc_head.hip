@@ -1917,7 +1917,7 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
             });
             if (p.splits > 1) launch_input_grad_sum<T>(c, dx, p.m, p.n, p.splits);
         }
-        if (rows <= kThin) {
+        if (few && rows <= kThin) {         // a last chunk of many rows may be as short, with two scaled planes of d
             launch_thin_weight<T>(c, {x, c.ldx, gains, static_cast<int32_t>(rows), cols, static_cast<int32_t>(count), d, l.d_plane, ldd, c.dw + first * c.hidden, accumulate, 0});
         } else if (few && rows <= kFewWeight) {
             launch_few_weight<T>(c, d_planes, count, {x, c.ldx, gains, c.dw + first * c.hidden, accumulate, 0});

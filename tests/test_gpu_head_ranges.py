@@ -1,0 +1,75 @@
+"""The head at the ends of what it accepts: numbers of tokens beyond what is taken together, widths and vocabularies beyond the usual,
+gradients of losses of very different size.  The oracle is the formulas in 64 bits, on the GPU; tolerances as in test_gpu_training."""
+import math
+
+import pytest
+import torch
+
+from paper_2312_17530_amd import binding as b
+from .test_gpu_training import BF16, F32, _close, _head_run
+
+pytestmark = pytest.mark.gpu
+
+
+def _case(rows, hidden, vocab, dtype, top=0, seed=0):
+    """Inputs made on the GPU; one row in five has no answer, entries of a teacher name a token twice now and then."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def rand(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    w = rand(vocab, hidden).mul_(2 / math.sqrt(hidden)).to(dtype)
+    case = dict(w=w, row_grad=0.01 * torch.rand(rows, generator=gen, device="cuda") - 0.002)
+    x = rand(rows, hidden)
+    if top == 0:
+        target = torch.randint(vocab, (rows,), generator=gen, device="cuda")
+        x[::2] += 3 * w[target[::2]].float()
+        target[torch.rand(rows, generator=gen, device="cuda") < 0.2] = -1
+        case["target"] = target.int()
+    else:
+        idx = torch.randint(vocab, (rows, top), generator=gen, device="cuda")
+        x[::2] += w[idx[::2, 0]].float()
+        idx[torch.rand(rows, generator=gen, device="cuda") < 0.2] = -1
+        case["top_idx"], case["top_logit"] = idx.int(), 4 * rand(rows, top)
+    case["x"] = x.to(dtype)
+    return case
+
+
+def _exact(case, t=1.0):
+    """Results in 64 bits, and the gradients' terms without cancellation."""
+    x, w, g = case["x"].double(), case["w"].double(), case["row_grad"].double()
+    rows, vocab = x.shape[0], w.shape[0]
+    logp = x @ w.t() / t
+    lse = torch.logsumexp(logp, 1)
+    logp -= lse[:, None]
+    q = torch.zeros_like(logp)
+    if "target" in case:
+        idx, share = case["target"][:, None].long(), torch.ones(rows, 1, dtype=torch.float64, device="cuda")
+        kept = (idx >= 0) & (idx < vocab)
+    else:
+        idx, logit = case["top_idx"].long(), case["top_logit"].double()
+        kept = (idx >= 0) & (idx < vocab) & (logit > -math.inf)
+        share = torch.softmax(torch.where(kept, logit / t, -math.inf), 1)
+    q.scatter_add_(1, idx.clamp(0, vocab - 1), torch.where(kept, share, 0.0))
+    has = kept.any(1)
+    loss = torch.where(has, t * t * (torch.special.xlogy(q, q) - q * logp).sum(1), 0.0)
+    g = torch.where(has, t * g, 0.0)[:, None]
+    p = logp.exp_()
+    d, both = (p - q) * g, (p + q) * g.abs()
+    x = torch.where(has[:, None], x, 0.0)
+    return dict(loss=loss, lse=lse, dx=d @ w, dw=d.t() @ x), dict(dx=both @ w.abs(), dw=both.t() @ x.abs())
+
+
+def _check(tag, case, t=1.0):
+    print("head", tag, flush=True)
+    got, (want, terms) = _head_run(case, t), _exact(case, t)
+    for k in got:
+        _close(f"{tag} {k}", got[k], want[k].cpu(), case["x"].dtype if k == "dx" else F32, terms[k].cpu() if k in terms else None)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("over", [1, 8, 9])
+def test_a_few_tokens_more_than_are_taken_together(over, top, dtype):
+    """16384 tokens go through the backward pass together; the rest of them, however few, are in the same form."""
+    _check(f"16384 + {over} rows, top {top}, {dtype}", _case(16384 + over, 40, 300, dtype, top, seed=over), 2.0 if top else 1.0)

@@ -1909,7 +1909,7 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
             }
             Problem p = problem(d_planes, wd, rows, c.hidden, count);
             Choice how = choose(rows, c.hidden, count, l.splits_most);
-            if (wide_dx(c.dtype, c.rows, c.hidden)) how = {kTileWide, std::min<int64_t>(l.splits_most, 512 / ((c.hidden + 255) / 256))};
+            if (wide_dx(c.dtype, c.rows, c.hidden)) how = {kTileWide, std::max<int64_t>(1, std::min<int64_t>(l.splits_most, 512 / ((c.hidden + 255) / 256)))};
             with_shape<D, false, true, false, FOR_DX, PLANES>(how.tile, [&](auto shape) {
                 using S = decltype(shape);
                 const dim3 grid = cut<S>(p, how.splits);

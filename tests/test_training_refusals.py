@@ -1,8 +1,12 @@
 """What the training operators refuse.  Arguments are checked before anything reaches the GPU, so this needs none: the addresses are
 numbers, and no kernel is launched."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
+import torch
 
 from paper_2312_17530_amd import binding as b
 
@@ -87,3 +91,30 @@ def test_workspace_sizes():
                         both, loss = (lib.rsdgc_head_workspace_bytes(dtype, rows, hidden, vocab, top, back) for back in (1, 0))
                         assert both >= loss > 0 and both % 256 == 0, (dtype, rows, hidden, vocab, top)
 
+
+
+# widths up to the widest, in every form
+WIDE = """
+import sys
+sys.path.insert(0, sys.argv[1])
+from paper_2312_17530_amd import binding as b
+from tests import test_training_refusals as t
+for dtype in (0, 1):
+    for rows in (1, 8, 9, 40, 64, 65, 300, 20000):
+        for hidden in (131072, 131080, 1 << 20):
+            for name, base in (("rsdgc_head_loss", t.HEAD), ("rsdgc_head_loss_backward", t.HEAD_BACK), ("rsdgc_distill_loss_backward", t.TAUGHT_BACK)):
+                far = dict(dtype=dtype, rows=rows, hidden=hidden, vocab=1000, ldx=hidden, ldw=hidden, lddx=hidden)
+                far |= {k: t.X + (i << 38) for i, k in enumerate(("x", "w", "dx", "dw", "ws", "target", "idx", "logit", "loss", "lse", "row_grad"))}
+                changes = {k: v for k, v in far.items() if k in base}
+                code = t._call(name, base, changes)
+                assert code == b.RSDGC_EHIP, (name, changes, code)
+print("all returned")
+"""
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="the addresses are numbers: only where no kernel can be launched")
+def test_the_widest_rows_return():
+    """Accepted sizes come back with the launch's error where there is no GPU; in a process of its own, which a fault would end."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    proc = subprocess.run([sys.executable, "-c", WIDE, root], capture_output=True, text=True, timeout=300)
+    assert proc.returncode == 0 and "all returned" in proc.stdout, (proc.returncode, proc.stderr[-2000:])

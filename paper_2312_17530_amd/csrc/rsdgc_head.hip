@@ -1997,7 +1997,7 @@ int forward(const Call &c, const char *what) {
 int backward(const Call &c, const char *what) {
     if (!inputs_ok(c) || !c.dw || !aligned_to(c.dw, 4)) return RSDGC_EINVAL;
     const size_t size = type_size(c.dtype);
-    if (c.rows > 0 && (!c.lse || !c.row_grad || !c.dx || c.lddx < c.hidden || !aligned_to(c.lse, 4) || !aligned_to(c.row_grad, 4) || !aligned_to(c.dx, size))) return RSDGC_EINVAL;
+    if (c.rows > 0 && (!c.lse || !c.row_grad || !c.dx || c.lddx < c.hidden || c.lddx > kMaxStride || !aligned_to(c.lse, 4) || !aligned_to(c.row_grad, 4) || !aligned_to(c.dx, size))) return RSDGC_EINVAL;
     const Layout l = layout_of(c.dtype, c.rows, c.hidden, c.vocab, c.top, true, as_is(c));
     Range read[6];
     Range (&four)[4] = *reinterpret_cast<Range (*)[4]>(read);

@@ -83,3 +83,24 @@ def test_a_few_tokens_more_than_are_taken_together(over, top, dtype):
 def test_wide_rows(rows, hidden, dtype):
     """Widths whose columns alone are more tiles of dx than the card has places for, and one whose vocabulary is cut into shares."""
     _check(f"{rows} rows of {hidden}, {dtype}", _case(rows, hidden, 203, dtype, seed=rows))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [30, 300])
+def test_rows_as_far_apart_as_they_may_be(rows, dtype):
+    """x, W and dx with 2^20 elements from one row to the next: the same bits as without gaps, and the gaps of dx as they were."""
+    case = _case(rows, 48, 203, dtype, seed=rows)
+    far = dict(case)
+    for k in ("x", "w"):
+        far[k] = torch.full((case[k].shape[0], 1 << 20), math.nan, dtype=dtype, device="cuda")[:, 512:560]
+        far[k].copy_(case[k])
+    out = torch.full((rows, 1 << 20), 7.0, dtype=dtype, device="cuda")
+    dx = out[:, 64:112]
+    want = _head_run(case)
+    loss, lse, dw = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(203, 48, device="cuda")
+    ws = torch.empty(b.rsdgc_head_workspace_bytes(dtype, rows, 48, 203), dtype=torch.uint8, device="cuda")
+    b.rsdgc_head_loss(far["x"], far["w"], far["target"], loss, lse, ws)
+    b.rsdgc_head_loss_backward(far["x"], far["w"], far["target"], lse, far["row_grad"], dx, dw, False, ws)
+    for k, got in dict(loss=loss, lse=lse, dx=dx, dw=dw).items():
+        assert torch.equal(got, want[k]), k
+    assert bool((out[:, :64] == 7.0).all()) and bool((out[:, 112:] == 7.0).all())

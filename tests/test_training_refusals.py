@@ -66,6 +66,13 @@ def test_refused(name, base, changes):
         assert _call(name, base, {**changes, "dtype": dtype}) == b.RSDGC_EINVAL, (dtype, changes)
 
 
+@pytest.mark.parametrize("name,base", [("rsdgc_head_loss_backward", HEAD_BACK), ("rsdgc_distill_loss_backward", TAUGHT_BACK)])
+@pytest.mark.parametrize("stride", [(1 << 20) + 1, 1 << 23, 1 << 40])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_rows_of_dx_too_far_apart_are_refused(name, base, stride, dtype):
+    assert _call(name, base, dict(dtype=dtype, lddx=stride)) == b.RSDGC_EINVAL
+
+
 @pytest.mark.parametrize("name,base", [("rsdgc_layer_norm", NORM), ("rsdgc_head_loss", HEAD), ("rsdgc_distill_loss", TAUGHT)])
 def test_no_rows_touch_nothing(name, base):
     # without rows no address of theirs is looked at, and nothing is launched

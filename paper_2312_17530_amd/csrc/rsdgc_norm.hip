@@ -24,7 +24,7 @@ constexpr int kMaxThreads = 1024;      // that share a row in the forward pass; 
 constexpr int kBackwardThreads = 512;  // ... in the backward pass, whose threads need more registers
 constexpr int kGroupThreads = 512;     // threads of a backward workgroup whose rows are narrower
 constexpr int kMaxLines = 512;         // lines of partial sums, two workgroups per CU
-constexpr int kForwardBlocks = 2048;   // workgroups of 256 threads that go over the rows in the forward pass, eight per CU
+constexpr int kForwardBlocks = 2048;   // workgroups of 256 threads that go over the rows in the forward pass, eight per CU; of the wide kernels'
 
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Chunk { T v[VEC]; };
 
@@ -139,22 +139,23 @@ __global__ __launch_bounds__(THREADS * GROUPS) void k_norm_forward(const Forward
 template <typename T>
 __global__ __launch_bounds__(kMaxThreads) void k_norm_forward_wide(const ForwardArgs<T> a) {
     __shared__ float red[kMaxThreads / 64];
-    const int64_t row = blockIdx.x;
-    const T *x = a.x + row * a.ldx;
-    float s = 0.0f;
-    for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) s += to_float(x[c]);
-    const float mean = row_sum<kMaxThreads>(s, red, 0) / static_cast<float>(a.cols);
-    float q = 0.0f;
-    for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) { const float d = to_float(x[c]) - mean; q = fmaf(d, d, q); }
-    const float rstd = 1.0f / sqrtf(row_sum<kMaxThreads>(q, red, 0) / static_cast<float>(a.cols) + a.eps);
-    if (threadIdx.x == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
-    }
-    T *y = a.y + row * a.ldy;
-    for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) {
-        const float unit = (to_float(x[c]) - mean) * rstd;
-        y[c] = static_cast<T>(fmaf(unit, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f));
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = a.x + row * a.ldx;
+        float s = 0.0f;
+        for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) s += to_float(x[c]);
+        const float mean = row_sum<kMaxThreads>(s, red, 0) / static_cast<float>(a.cols);
+        float q = 0.0f;
+        for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) { const float d = to_float(x[c]) - mean; q = fmaf(d, d, q); }
+        const float rstd = 1.0f / sqrtf(row_sum<kMaxThreads>(q, red, 0) / static_cast<float>(a.cols) + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        T *y = a.y + row * a.ldy;
+        for (int c = threadIdx.x; c < a.cols; c += kMaxThreads) {
+            const float unit = (to_float(x[c]) - mean) * rstd;
+            y[c] = static_cast<T>(fmaf(unit, a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f));
+        }
     }
 }
 
@@ -388,7 +389,7 @@ bool rows_in_16(const void *p, int64_t ld, int64_t cols, size_t size) {
 template <typename T>
 void forward_typed(const ForwardArgs<T> &a, hipStream_t s) {
     if (threads_per_row(a.cols) > kMaxThreads)
-        hipLaunchKernelGGL((k_norm_forward_wide<T>), dim3(static_cast<unsigned>(a.rows)), dim3(kMaxThreads), 0, s, a);
+        hipLaunchKernelGGL((k_norm_forward_wide<T>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kForwardBlocks))), dim3(kMaxThreads), 0, s, a);
     else if (rows_in_16(a.x, a.ldx, a.cols, sizeof(T)) && rows_in_16(a.y, a.ldy, a.cols, sizeof(T)))
         forward_vec<T, 16 / sizeof(T)>(a, s);
     else

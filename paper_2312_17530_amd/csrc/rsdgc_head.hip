@@ -132,10 +132,11 @@ __device__ __forceinline__ bool row_answers(const Teacher &a, int64_t row, int32
 __global__ __launch_bounds__(256) void k_answers(const Teacher a, int64_t rows, int32_t *idx, float *q, const float *row_grad, float t, float *gain) {
     extern __shared__ int32_t lds_answers[];       // [4][2][top]
     const int wave = threadIdx.x >> 6;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    if (row >= rows) return;
-    const bool any = row_answers(a, row, lds_answers + wave * 2 * a.top, idx + row * a.top, q + row * a.top);
-    if (gain && (threadIdx.x & 63) == 0) gain[row] = any ? t * row_grad[row] : 0.0f;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave; row < rows; row += static_cast<int64_t>(gridDim.x) * 4) {
+        const bool any = row_answers(a, row, lds_answers + wave * 2 * a.top, idx + row * a.top, q + row * a.top);
+        if (gain && (threadIdx.x & 63) == 0) gain[row] = any ? t * row_grad[row] : 0.0f;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // the room has been read
+    }
 }
 
 // ------------------------------------------------------------------- planes
@@ -1656,9 +1657,10 @@ Picked picked_by(const Call &c, const Layout &l, int64_t first_row, int64_t firs
 Teacher teacher_of(const Call &c, int64_t first_row) {
     return {c.idx + first_row * c.top, c.logit + first_row * c.top, c.top, static_cast<int32_t>(c.vocab), 1.0f / c.t};
 }
+constexpr int64_t kAnswerBlocks = int64_t(1) << 20;      // a launch has less than 2^32 threads
 size_t answer_room(const Call &c) { return static_cast<size_t>(c.top) * 32; }      // LDS of four waves
 void launch_answers(const Call &c, const Layout &l, bool backward) {
-    hipLaunchKernelGGL(k_answers, dim3(static_cast<unsigned>((c.rows + 3) / 4)), dim3(256), answer_room(c), c.stream, teacher_of(c, 0), c.rows, in_ws<int32_t>(c, l.idx),
+    hipLaunchKernelGGL(k_answers, dim3(blocks_for((c.rows + 3) / 4, kAnswerBlocks)), dim3(256), answer_room(c), c.stream, teacher_of(c, 0), c.rows, in_ws<int32_t>(c, l.idx),
                        in_ws<float>(c, l.q), c.row_grad, c.t, backward ? in_ws<float>(c, l.gain) : static_cast<float *>(nullptr));
 }
 

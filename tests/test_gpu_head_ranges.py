@@ -104,3 +104,44 @@ def test_rows_as_far_apart_as_they_may_be(rows, dtype):
     for k, got in dict(loss=loss, lse=lse, dx=dx, dw=dw).items():
         assert torch.equal(got, want[k]), k
     assert bool((out[:, :64] == 7.0).all()) and bool((out[:, 112:] == 7.0).all())
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_more_rows_behind_a_teacher_than_a_launch_has_waves(backward):
+    """2^26 and a few tokens of width 1 over three words: a wave for each token would be 2^32 threads.  The tokens repeat, so that a few
+    of them tell all."""
+    rows, kinds = (1 << 26) + 5, 7
+    small = _case(kinds, 1, 3, BF16, 1, seed=2)
+    small["top_idx"][:, 0] = torch.tensor([0, 1, 2, -1, 2, 0, 1], device="cuda")
+    at = torch.arange(rows, device="cuda", dtype=torch.int32) % kinds
+    x, idx, logit, grad = (small[k].index_select(0, at) for k in ("x", "top_idx", "top_logit", "row_grad"))
+    loss, lse = torch.full((rows,), 7.0, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    ws = torch.empty(b.rsdgc_head_workspace_bytes(BF16, rows, 1, 3, 1, backward), dtype=torch.uint8, device="cuda")
+    want, _ = _exact(small, 2.0)
+    b.rsdgc_distill_loss(x, small["w"], idx, logit, 2.0, loss, lse, ws)
+    got = dict(loss=loss, lse=lse)
+    if backward:
+        got["dx"], dw = torch.empty_like(x), torch.empty(3, 1, device="cuda")
+        b.rsdgc_distill_loss_backward(x, small["w"], idx, logit, 2.0, lse, grad, got["dx"], dw, False, ws)
+        times = torch.bincount(at, minlength=kinds).double()
+        d = want["dx"].new_tensor(0.0)
+        for n in range(kinds):
+            one = {k: small[k][n:n + 1] for k in ("x", "top_idx", "top_logit", "row_grad")}
+            d = d + times[n] * _exact(one | dict(w=small["w"]), 2.0)[0]["dw"]
+        # 16384 terms at a time, sqrt(16384) roundings of 2^-24, and 4096 sums of these one after another, much alike, so that their
+        # roundings may all have one sign: half of 4096, the sum growing evenly
+        assert float((dw.double() - d).norm()) <= (128 + 2048) * 2.0 ** -24 * float((times[:, None] * _rows_of(small)).abs().sum())
+    for k, v in got.items():
+        for n in range(kinds):
+            mine = v.view(-1)[n::kinds]
+            assert bool((mine == mine[0]).all()), (k, n)
+        _close(k, v[:kinds], want[k].cpu(), BF16 if k == "dx" else F32)
+
+
+def _rows_of(case):
+    """|d| |x| of each token, summed over the vocabulary."""
+    out = []
+    for n in range(case["x"].shape[0]):
+        one = {k: case[k][n:n + 1] for k in ("x", "top_idx", "top_logit", "row_grad")}
+        out.append(_exact(one | dict(w=case["w"]), 2.0)[1]["dw"].sum())
+    return torch.stack(out)[:, None]

@@ -1461,6 +1461,8 @@ constexpr int kStep = 64;              // k in whose multiples the k axis is cut
 // with a deep ring, for products with little to do.  64 x 256 with a deep ring: dx of up to 64 rows, which reads W across its rows,
 // 512 bytes of each instead of 128.
 enum Tile { kTile64, kTile128, kTile256, kTileWide };
+constexpr int64_t kSide[] = {64, 128, 256};        // of the square ones
+constexpr int64_t kMaxTiles = int64_t(1) << 22;    // of a launch, up to 512 threads each
 struct Choice {
     Tile tile;
     int64_t splits;
@@ -1473,7 +1475,7 @@ Choice choose(int64_t m, int64_t n, int64_t k, int64_t splits_most, Tile largest
     Choice best = {};
     double least = 0.0;
     for (int tile = kTile64; tile <= largest; ++tile) {
-        static constexpr int64_t kSide[] = {64, 128, 256}, kRoom[] = {512, 512, 256};
+        static constexpr int64_t kRoom[] = {512, 512, 256};
         static constexpr double kUnits[] = {3.0, 5.0, 8.0};
         const int64_t t = kSide[tile], room = kRoom[tile], steps = (k + kStep - 1) / kStep;
         if (tile > kTile64 && std::min(m, n) <= t / 2) break;         // half of it and more would be beyond the edge
@@ -1570,6 +1572,10 @@ Layout layout_of(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, int
     if (backward) l.piece = std::min(l.piece, d_cols);
     l.stats_tile = l.direct ? kTile64 : choose(vocab, std::max<int64_t>(1, l.rows), hidden, 1).tile;      // direct: strips of 32 too
     l.strips = static_cast<int32_t>((vocab + kStripOf[l.stats_tile] - 1) / kStripOf[l.stats_tile]);
+    if (!backward && !l.direct) {
+        const int64_t side = kSide[l.stats_tile], across = (std::max<int64_t>(1, l.rows) + side - 1) / side;
+        l.piece = std::min(l.piece, std::max<int64_t>(256, kMaxTiles / across * side / 256 * 256));
+    }
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += static_cast<size_t>(up(bytes, 256)); return here; };
     l.scales = take(kScales * 4);

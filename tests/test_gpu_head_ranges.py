@@ -145,3 +145,25 @@ def _rows_of(case):
         one = {k: case[k][n:n + 1] for k in ("x", "top_idx", "top_logit", "row_grad")}
         out.append(_exact(one | dict(w=case["w"]), 2.0)[1]["dw"].sum())
     return torch.stack(out)[:, None]
+
+
+def test_more_logits_than_a_launch_has_tiles():
+    """65536 tokens over 8.4 million words of width 8, tiles of 256 x 256 and 512 threads: 2^32 threads and a few more.  64 of the tokens
+    are compared."""
+    rows, hidden, vocab = 65536, 8, (1 << 23) + 77
+    size = b.rsdgc_head_workspace_bytes(BF16, rows, hidden, vocab, 0, False)
+    if torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved() < size + (24 << 30):
+        pytest.skip(f"{(size >> 30) + 24} GiB of memory are needed")
+    torch.cuda.empty_cache()
+    case = _case(rows, hidden, vocab, BF16, seed=3)
+    loss, lse = torch.full((rows,), 7.0, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    b.rsdgc_head_loss(case["x"], case["w"], case["target"], loss, lse, torch.empty(size, dtype=torch.uint8, device="cuda"))
+    at = torch.arange(0, rows, rows // 63, device="cuda")[:64]
+    z = case["x"][at].double() @ case["w"].double().t()
+    target = case["target"][at].long()
+    want = torch.logsumexp(z, 1)
+    _close("lse", lse[at], want.cpu(), F32)
+    own = z[torch.arange(len(at), device="cuda"), target.clamp(min=0)]
+    _close("loss", loss[at], torch.where(target >= 0, want - own, 0.0).cpu(), F32)
+    del z
+    torch.cuda.empty_cache()

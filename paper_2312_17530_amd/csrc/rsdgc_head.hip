@@ -96,7 +96,7 @@ __device__ __forceinline__ bool row_answers(const Teacher &a, int64_t row, int32
     float most = -INFINITY;
     for (int k = lane; k < top; k += 64) {
         const int32_t i = a.idx[row * top + k];
-        const float l = a.logit[row * top + k] * a.inv_t;
+        const float l = a.logit[row * top + k];
         const bool counts = i >= 0 && i < a.vocab && l > -INFINITY;     // NaN: no
         at[k] = counts ? i : -1;
         e[k] = l;
@@ -105,8 +105,9 @@ __device__ __forceinline__ bool row_answers(const Teacher &a, int64_t row, int32
     most = wave_max(most);
     float sum = 0.0f;
     for (int k = lane; k < top; k += 64) {
-        // a teacher that is certain (an infinite logit) splits its certainty among those
-        e[k] = at[k] < 0 ? 0.0f : most == INFINITY ? (e[k] == INFINITY ? 1.0f : 0.0f) : exp2f((e[k] - most) * kLog2e);
+        // a teacher that is certain (an infinite logit) splits its certainty among those; the temperature comes after the difference, so
+        // that float32's lowest and largest values stay what they are
+        e[k] = at[k] < 0 ? 0.0f : most == INFINITY ? (e[k] == INFINITY ? 1.0f : 0.0f) : exp2f((e[k] - most) * a.inv_t * kLog2e);
         sum += e[k];
     }
     sum = wave_sum(sum);

@@ -167,3 +167,19 @@ def test_more_logits_than_a_launch_has_tiles():
     _close("loss", loss[at], torch.where(target >= 0, want - own, 0.0).cpu(), F32)
     del z
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t", [0.25, 1.0, 3.0])
+@pytest.mark.parametrize("rows", [20, 900])
+def test_teacher_logits_at_the_ends_of_float32(rows, t, dtype):
+    """Entries at the type's lowest value count like any others, a row of nothing else is an even answer; the largest ones do not
+    become infinite by the temperature."""
+    case = _case(rows, 64, 200, dtype, 5, seed=rows)
+    low, high = torch.finfo(F32).min, torch.finfo(F32).max
+    case["top_idx"][:] = torch.tensor([3, 50, 7, 199, 120], device="cuda")
+    case["top_logit"][0::4, 2:] = low                  # masked ones beside ordinary ones
+    case["top_logit"][1::4] = low                      # nothing but masked ones
+    case["top_logit"][2::4, 1:3] = high                # two share everything
+    case["top_logit"][2::4, 3] = high * 0.75
+    _check(f"{rows} rows, t {t}, {dtype}", case, t)

@@ -476,7 +476,7 @@ int rsdgc_head_loss_backward(int32_t dtype, int64_t rows, int64_t hidden, int64_
  *   top_idx, top_logit [device] int32 / float32 [rows][top], 1 <= top <= RSDGC_MAX_TOP, in any order.
  *           An entry counts where 0 <= top_idx < vocab and its logit is above -inf (and no NaN); entries
  *           that name the same token add up; a row where none counts has loss +0 and no gradient.
- *   temperature  finite, above 0.
+ *   temperature  finite, above 0, and so is its reciprocal in float32.
  * Otherwise as rsdgc_head_loss.  The backward pass has d[n][v] = t (exp(z - lse[n]) - q_v) * row_grad[n]. */
 #define RSDGC_MAX_TOP 1024
 int rsdgc_distill_loss(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, const void *x, int64_t ldx, const void *w,

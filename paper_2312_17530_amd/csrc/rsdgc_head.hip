@@ -1962,7 +1962,7 @@ bool apart(const Range *written, int n_written, const Range *read, int n_read) {
 bool inputs_ok(const Call &c) {
     const size_t size = type_size(c.dtype);
     if (!sizes_ok(c.dtype, c.rows, c.hidden, c.vocab) || c.ldx < c.hidden || c.ldw < c.hidden || c.ldx > kMaxStride || c.ldw > kMaxStride) return false;
-    if (c.top < 0 || c.top > RSDGC_MAX_TOP || !std::isfinite(c.t) || !(c.t > 0.0f)) return false;
+    if (c.top < 0 || c.top > RSDGC_MAX_TOP || !std::isfinite(c.t) || !(c.t > 0.0f) || !std::isfinite(1.0f / c.t)) return false;
     if (!c.w || !aligned_to(c.w, size) || !c.ws || !aligned_to(c.ws, 256)) return false;
     if (c.rows == 0) return true;
     return c.x && aligned_to(c.x, size) && c.idx && aligned_to(c.idx, 4) && (c.top == 0 || (c.logit && aligned_to(c.logit, 4)));

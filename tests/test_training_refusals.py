@@ -125,3 +125,9 @@ def test_the_widest_rows_return():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     proc = subprocess.run([sys.executable, "-c", WIDE, root], capture_output=True, text=True, timeout=300)
     assert proc.returncode == 0 and "all returned" in proc.stdout, (proc.returncode, proc.stderr[-2000:])
+
+
+@pytest.mark.parametrize("name,base", [("rsdgc_distill_loss", TAUGHT), ("rsdgc_distill_loss_backward", TAUGHT_BACK)])
+@pytest.mark.parametrize("t", [2e-39, 1e-45])
+def test_a_temperature_without_a_reciprocal_is_refused(name, base, t):
+    assert _call(name, base, dict(t=t)) == b.RSDGC_EINVAL

@@ -563,7 +563,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_loss(const T *x, i
     l = 0.0f;
     for (int u = 0; u < WAVES; ++u) l += part[u];
     if (wave == 0 && lane == 0) {
-        loss[row] = t * t * l;
+        loss[row] = t * (t * l);                   // the square may leave the range
         lse_out[row] = lse;
     }
 }

@@ -183,3 +183,15 @@ def test_teacher_logits_at_the_ends_of_float32(rows, t, dtype):
     case["top_logit"][2::4, 1:3] = high                # two share everything
     case["top_logit"][2::4, 3] = high * 0.75
     _check(f"{rows} rows, t {t}, {dtype}", case, t)
+
+
+@pytest.mark.parametrize("rows", [20, 900])
+def test_a_temperature_whose_square_is_beyond_float32(rows):
+    """Logits that are almost nothing: rows without an answer have loss +0 all the same, the statistics are those of even words."""
+    case = _case(rows, 64, 200, F32, 5, seed=rows)
+    case["top_idx"][::3] = -1
+    got, (want, _) = _head_run(case, 1e20), _exact(case, 1e20)
+    none = (case["top_idx"] < 0).all(1)
+    assert bool((got["loss"][none] == 0.0).all()) and not bool(torch.isnan(got["loss"]).any())
+    _close("lse", got["lse"], want["lse"].cpu(), F32)
+    assert bool((got["dx"][none] == 0.0).all())

@@ -16,9 +16,10 @@
 //              Three products (lo*lo is under 2^-22 of hi*hi), and a pass over the operand to find s.
 //                float32   x, W and d as two planes
 //                bfloat16  logits from x and W as they are; dW from d as two planes and x as one (its 8 bits fit), because dW
-//                          goes to a float32 arena; dx, bfloat16 itself, from d's hi plane and W as one plane: 11 bits of d are
-//                          enough for it and 8 are not (a confident token's d is one large entry, whose rounding reaches the
-//                          whole row)
+//                          goes to a float32 arena; dx from d as two planes and W as one.  dx is bfloat16 itself, yet 11 bits of
+//                          d are not enough: a token's d sums up to nothing, so that what W's rows have in common leaves dx but
+//                          for the roundings of d (a shared part a hundred times the rest: dx 2e-2 off with 11 bits, 1.7e-3, its
+//                          own rounding, with 22)
 //   few rows   bfloat16, three planes of 8 bits each, which keep float32's range and need no scale.  Six products for two
 //              operands of three planes; x and W in bfloat16 are taken as they are.  More products, but these are hidden behind
 //              the reading of W, and W is not gone over beforehand: float32 W is split on its way from memory to registers.
@@ -1519,7 +1520,7 @@ dim3 cut(Problem &p, int64_t splits) {
 template <typename V, bool A_MC, bool B_MC, bool PAIRED, int PA, int PB, typename F>
 void with_shape(Tile tile, F &&f) {
     if (tile == kTile64) return f(typename ShapeOf<kTile64, V, A_MC, B_MC, PAIRED, PA, PB>::S{});
-    if constexpr (!A_MC && B_MC && PA == 2 && PB == 1)
+    if constexpr (!A_MC && B_MC && PA == 2 && PB == 1 && std::is_same<V, bfloat8>::value)       // few rows
         if (tile == kTileWide) return f(typename ShapeOf<kTileWide, V, A_MC, B_MC, PAIRED, PA, PB>::S{});
     if constexpr (PA < 3) {
         if (tile == kTile128) return f(typename ShapeOf<kTile128, V, A_MC, B_MC, PAIRED, PA, PB>::S{});
@@ -1870,8 +1871,8 @@ void launch_few_weight(const Call &c, const Operand &d, int64_t count, const Few
     else go(integral_constant<int, 8>{}, integral_constant<int, kWide ? 1 : 2>{});
 }
 
-// V: type of the logits' operands, PLANES: of these; D: type of d's planes, D_PLANES: of these, FOR_DX: of those for dx.
-template <typename T, typename V, int PLANES, typename D, int D_PLANES, int FOR_DX>
+// V: type of the logits' operands, PLANES: of these; D: type of d's planes, D_PLANES: of these.
+template <typename T, typename V, int PLANES, typename D, int D_PLANES>
 void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t rows, bool accumulate) {
     const bool wide = c.dtype == RSDGC_F32, few = l.few, x_as_is = takes_as_is(c.dtype, c.x, c.ldx, c.hidden), w_as_is = takes_as_is(c.dtype, c.w, c.ldw, c.hidden);
     const int cols = static_cast<int>(c.hidden), ld = static_cast<int>(l.ld);
@@ -1919,7 +1920,8 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
             Problem p = problem(d_planes, wd, rows, c.hidden, count);
             Choice how = choose(rows, c.hidden, count, l.splits_most);
             if (wide_dx(c.dtype, c.rows, c.hidden)) how = {kTileWide, std::max<int64_t>(1, std::min<int64_t>(l.splits_most, 512 / ((c.hidden + 255) / 256)))};
-            with_shape<D, false, true, false, FOR_DX, PLANES>(how.tile, [&](auto shape) {
+            constexpr int kForDx = D_PLANES == 3 ? 2 : D_PLANES;      // bfloat16: the third plane is below what dx can hold
+            with_shape<D, false, true, false, kForDx, PLANES>(how.tile, [&](auto shape) {
                 using S = decltype(shape);
                 const dim3 grid = cut<S>(p, how.splits);
                 hipLaunchKernelGGL((k_input_grad<S, T>), grid, dim3(S::kThreads), 0, c.stream, p, dx);
@@ -2023,11 +2025,11 @@ int backward(const Call &c, const char *what) {
             const int64_t rows = std::min(l.rows, c.rows - first);
             const bool accumulate = c.accumulate || first > 0;
             if (c.dtype == RSDGC_BF16) {
-                if (l.few) launch_backward<bf16, bfloat8, 1, bfloat8, 3, 2>(c, l, first, rows, accumulate);
-                else launch_backward<bf16, bfloat8, 1, half8, 2, 1>(c, l, first, rows, accumulate);
+                if (l.few) launch_backward<bf16, bfloat8, 1, bfloat8, 3>(c, l, first, rows, accumulate);
+                else launch_backward<bf16, bfloat8, 1, half8, 2>(c, l, first, rows, accumulate);
             } else {
-                if (l.few) launch_backward<float, bfloat8, 3, bfloat8, 3, 3>(c, l, first, rows, accumulate);
-                else launch_backward<float, half8, 2, half8, 2, 2>(c, l, first, rows, accumulate);
+                if (l.few) launch_backward<float, bfloat8, 3, bfloat8, 3>(c, l, first, rows, accumulate);
+                else launch_backward<float, half8, 2, half8, 2>(c, l, first, rows, accumulate);
             }
         }
     }

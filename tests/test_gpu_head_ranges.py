@@ -195,3 +195,16 @@ def test_a_temperature_whose_square_is_beyond_float32(rows):
     assert bool((got["loss"][none] == 0.0).all()) and not bool(torch.isnan(got["loss"]).any())
     _close("lse", got["lse"], want["lse"].cpu(), F32)
     assert bool((got["dx"][none] == 0.0).all())
+
+
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("dtype,rows,hidden,vocab", [(BF16, 100, 64, 900), (BF16, 100, 61, 900), (BF16, 700, 64, 900), (BF16, 700, 61, 900), (BF16, 2100, 520, 5003), (F32, 700, 64, 900)])
+def test_words_that_are_much_alike(dtype, rows, hidden, vocab, top):
+    """Embeddings share a direction that is a hundred times what tells them apart.  A token's d sums up to nothing, so the shared part
+    leaves dx but for the roundings of d, which count a hundredfold: as many of its bits as float32 results need."""
+    case = _case(rows, hidden, vocab, dtype, top, seed=hidden)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    shared = torch.randn(hidden, generator=gen, device="cuda")
+    case["w"].copy_(shared + 0.01 * torch.randn(vocab, hidden, generator=gen, device="cuda"))
+    case["x"].copy_(torch.randn(rows, hidden, generator=gen, device="cuda"))
+    _check(f"alike {rows}x{hidden}x{vocab} top {top} {dtype}", case, 2.0 if top else 1.0)

@@ -455,8 +455,8 @@ size_t rsdgc_layer_norm_workspace_bytes(int64_t rows, int64_t cols);   /* 0: bad
  *   loss, lse [device] float32[rows]; lse of every row.
  *   workspace [device] rsdgc_head_workspace_bytes bytes, 256-byte aligned.
  * float32 operands count with every bit where there are few rows, else with 22 bits of every
- * element (and an absolute error of 2^-40 of the largest finite magnitude of x, of W's piece);
- * products are summed in float32; an infinity in a float32 W may come out as NaN.    */
+ * element (and an absolute error of 2^-40 of the largest finite magnitude of the row of x, of W's
+ * piece); products are summed in float32; an infinity in a float32 W may come out as NaN.    */
 int rsdgc_head_loss(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, const void *x, int64_t ldx, const void *w,
                     int64_t ldw, const int32_t *target, float *loss, float *lse, void *workspace, void *stream);
 
@@ -465,6 +465,9 @@ int rsdgc_head_loss(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, 
  *   lse       [device] as rsdgc_head_loss left it.
  *   row_grad  [device] float32[rows]: the gradient of each row's loss (1 / count for a mean).
  *   dx        [device] rows x hidden of dtype,  dw [device] float32, vocab x hidden without gaps.
+ * Each element of d counts with 22 bits (in dx of few bfloat16 rows with 16) down to 2^-40 of the
+ * row's largest, whatever the other rows' row_grad is; in dw of many rows row_grad * x counts with
+ * 22 bits (bfloat16: as it is) down to 2^-40 of the largest of the call's rows.
  * rows = 0 zeroes dw, or leaves it with accumulate.                                  */
 int rsdgc_head_loss_backward(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, const void *x, int64_t ldx,
                              const void *w, int64_t ldw, const int32_t *target, const float *lse, const float *row_grad,

@@ -14,6 +14,9 @@
 //   many rows  float16, hi = f16(s a) and lo = f16(s a - hi), with a power of two s that brings the largest magnitude to
 //              2^14 .. 2^15: 22 bits of every element down to 2^-17 of the largest, below that an absolute error of 2^-40 of it.
 //              Three products (lo*lo is under 2^-22 of hi*hi), and a pass over the operand to find s.
+//              "Largest" is of a row for x under the logits, of a piece for W, of a token for d.  A token's gain g = m 2^e goes
+//              apart: d has m, dx's row 2^e at the end, and x under dW 2^e beforehand, with one scale over the rows; so no token
+//              knows how large another's gradient or x is, but for the sum over tokens, dW.
 //                float32   x, W and d as two planes
 //                bfloat16  logits from x and W as they are; dW from d as two planes and x as one (its 8 bits fit), because dW
 //                          goes to a float32 arena; dx from d as two planes and W as one.  dx is bfloat16 itself, yet 11 bits of
@@ -55,8 +58,10 @@ constexpr int64_t kMaxPiece = int64_t(1) << 24;       // its rows: those of a ti
 constexpr int64_t kPackBytes = int64_t(256) << 20;    // a piece of W laid out as planes
 constexpr int64_t kPackBytesRare = int64_t(64) << 20; // the same where only an unaligned W needs it
 
-// Scales of one backward pass, each a power of two.
-enum Scale { kScaleX, kScaleD, kScaleW, kScales = 16 };
+// Scales are powers of two, kept as exponents: those of x under the products of dW, of a piece of W.
+enum Shift { kShiftX, kShiftW, kShifts = 16 };
+constexpr int kTop = 14;                           // the exponent that a scale brings the largest magnitude to: 2^14 .. 2^15
+constexpr float kNoExponent = -10000.0f;           // of nothing
 
 // Up to so many rows a call takes the form for few rows.  Measured, few / many, us, W of 32768 rows (as is: both read as they lie):
 //   loss alone                     with gradients
@@ -146,12 +151,15 @@ __device__ __forceinline__ float finite_magnitude(float v) {
     const float m = fabsf(v);
     return m < INFINITY ? m : 0.0f;
 }
-// 2^e with which `most` comes to 2^14 .. 2^15; 1 for 0.
-__device__ __forceinline__ float scale_for(float most) {
-    if (!(most > 0.0f)) return 1.0f;
-    const int e = 15 - ilogbf(most) - 1;
-    return ldexpf(1.0f, min(126, max(-126, e)));
-}
+// |v| = m * 2^e with 1 <= m < 2; 0 for zero, infinities and NaN.
+__device__ __forceinline__ int exponent_of(float v) { return v != 0.0f && fabsf(v) < INFINITY ? ilogbf(v) : 0; }
+// The same of the largest of several magnitudes, as a float; kNoExponent for 0.
+__device__ __forceinline__ float exponent_of_most(float most) { return most > 0.0f ? static_cast<float>(ilogbf(most)) : kNoExponent; }
+// The exponent of the scale that brings magnitudes up to 2^most to kTop.
+__device__ __forceinline__ int shift_for(float most) { return most > kNoExponent ? kTop - static_cast<int>(most) : 0; }
+// A token's gain as it counts in d of many rows, with an exponent of its own: d then has all its bits whatever the other tokens' gains are,
+// and the rest of the gain, 2^(exponent_of(gain) - kTop), is taken up by dx's row and by x under dW.
+__device__ __forceinline__ float gain_in_d(float gain) { return ldexpf(gain, kTop - exponent_of(gain)); }
 __device__ __forceinline__ float block_max(float v, float *red) {
     v = wave_max(v);
     __syncthreads();
@@ -175,7 +183,7 @@ __device__ __forceinline__ void load_chunk(const T *row, int c, int cols, float 
     }
 }
 
-// The largest finite magnitude of a matrix; a partial result per workgroup.  Bound by memory: 16384 x 4096 bfloat16, a piece of W,
+// The exponent of the largest finite magnitude of a matrix; a partial result per workgroup.  Bound by memory: 16384 x 4096 bfloat16, a piece of W,
 // 38.7 us = 3.5 TB/s (16 bytes a thread, no atomics: a search's order must not matter).
 template <typename T>
 __global__ __launch_bounds__(256) void k_largest(const T *x, int64_t rows, int32_t cols, int64_t ld, float *parts) {
@@ -198,7 +206,7 @@ __global__ __launch_bounds__(256) void k_largest(const T *x, int64_t rows, int32
         if (c >= chunks) { c -= chunks; ++r; }
     }
     most = block_max(most, red);
-    if (threadIdx.x == 0) parts[blockIdx.x] = most;
+    if (threadIdx.x == 0) parts[blockIdx.x] = exponent_of_most(most);
 }
 
 // t * g_n of the rows: from an array, or (one target a row, t = 1) as they are needed.
@@ -213,35 +221,6 @@ struct Gains {
     }
 };
 
-// The backward pass's gain of each row, t * g_n, +0 for rows without an answer (whatever g_n holds there); the largest finite
-// magnitudes of x in the rows that have one, and of the gain.  parts: [2][workgroup].
-template <typename T>
-__global__ __launch_bounds__(256) void k_gain(const Answers a, const float *row_grad, float t, const T *x, int64_t rows, int32_t cols, int64_t ld, float *gain, float *parts) {
-    __shared__ float red[4];
-    float most_x = 0.0f, most_g = 0.0f;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        bool mine = false;
-        for (int k = threadIdx.x; k < a.top; k += 256) {
-            const int32_t i = a.idx[r * a.top + k];
-            mine |= i >= 0 && i < a.vocab;
-        }
-        const bool any = __syncthreads_or(mine);
-        const float g = any ? t * row_grad[r] : 0.0f;
-        if (threadIdx.x == 0) gain[r] = g;
-        most_g = fmaxf(most_g, finite_magnitude(g));
-        if (g == 0.0f) continue;
-        for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
-            float v[8];
-            load_chunk(x + r * ld, c, cols, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most_x = fmaxf(most_x, finite_magnitude(v[e]));
-        }
-    }
-    most_x = block_max(most_x, red);
-    most_g = block_max(most_g, red);
-    if (threadIdx.x == 0) { parts[blockIdx.x] = most_x; parts[gridDim.x + blockIdx.x] = most_g; }
-}
-
 template <typename H>
 __device__ __forceinline__ void split(float v, H &hi, H &lo) {
     hi = static_cast<H>(v);
@@ -251,22 +230,17 @@ __device__ __forceinline__ void split(float v, H &hi, H &lo) {
 __device__ __forceinline__ uint16_t bits(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
 __device__ __forceinline__ uint16_t bits(bf16 v) { return __builtin_bit_cast(uint16_t, v); }
 
-// A matrix as float16 planes with the scale that `parts` gives (hi, and lo where it is wanted), rows of `ld_out` (a multiple
-// of 8) elements, zeros beyond cols and in rows whose gain is 0.  The gain's scale comes from the parts behind (gain not NULL).
+// A matrix as float16 planes under the scale that `parts` gives (hi, and lo where it is wanted), rows of `ld_out` (a multiple
+// of 8) elements, zeros beyond cols.  gain not NULL: each row times the power of two of its gain, zeros where the gain is 0.
 // Bound by memory: 16384 x 4096 bfloat16 to one plane 42 us = 6.4 TB/s, its reads still in the cache from the search before.
 template <typename T>
 __global__ __launch_bounds__(256) void k_planes(const T *x, int64_t rows, int32_t cols, int64_t ld, const float *gain, const float *parts, int32_t n_parts,
-                                                float *scale_out, float *scale_gain, uint16_t *hi, uint16_t *lo, int32_t ld_out) {
+                                                int32_t *shift_out, uint16_t *hi, uint16_t *lo, int32_t ld_out) {
     __shared__ float red[4];
-    float most = 0.0f, most_g = 0.0f;
+    float most = kNoExponent;
     for (int i = threadIdx.x; i < n_parts; i += 256) most = fmaxf(most, parts[i]);
-    const float s = scale_for(block_max(most, red));
-    if (gain && blockIdx.x == 0) {
-        for (int i = threadIdx.x; i < n_parts; i += 256) most_g = fmaxf(most_g, parts[n_parts + i]);
-        most_g = block_max(most_g, red);
-        if (threadIdx.x == 0) *scale_gain = scale_for(most_g);
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *scale_out = s;
+    const int shift = shift_for(block_max(most, red));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *shift_out = shift;
     const int chunks = ld_out / 8;
     int64_t r = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / chunks;
     int c = static_cast<int>((static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) % chunks);
@@ -276,12 +250,13 @@ __global__ __launch_bounds__(256) void k_planes(const T *x, int64_t rows, int32_
     while (r < rows) {
         float v[8];
         load_chunk(x + r * ld, 8 * c, cols, v);
-        const bool in = !gain || gain[r] != 0.0f;
+        const float g = gain ? gain[r] : 1.0f;
+        const int by = shift + exponent_of(g);
         uint16_t h8[8], l8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
-            split(in ? v[e] * s : 0.0f, h, l);
+            split(g != 0.0f ? ldexpf(v[e], by) : 0.0f, h, l);
             h8[e] = bits(h);
             l8[e] = bits(l);
         }
@@ -293,33 +268,66 @@ __global__ __launch_bounds__(256) void k_planes(const T *x, int64_t rows, int32_
     }
 }
 
-// The same with a scale for each row (the forward pass: a row that nobody asks for does not coarsen the others).
-__global__ __launch_bounds__(256) void k_planes_by_row(const float *x, int32_t cols, int64_t ld, float *scale_out, uint16_t *hi, uint16_t *lo, int32_t ld_out) {
-    __shared__ float red[4];
-    const int64_t r = blockIdx.x;
+// By a workgroup: a thread's part of a row's largest finite magnitude, and the row as planes under a scale of its own.
+template <typename T>
+__device__ __forceinline__ float largest_of_row(const T *x, int cols) {
     float most = 0.0f;
     for (int c = threadIdx.x * 8; c < cols; c += 256 * 8) {
         float v[8];
-        load_chunk(x + r * ld, c, cols, v);
+        load_chunk(x, c, cols, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_magnitude(v[e]));
     }
-    const float s = scale_for(block_max(most, red));
-    if (threadIdx.x == 0) scale_out[r] = s;
+    return most;
+}
+template <typename T>
+__device__ __forceinline__ void row_as_planes(const T *x, int cols, int shift, int32_t *shift_out, uint16_t *hi, uint16_t *lo, int ld_out) {
+    if (threadIdx.x == 0) *shift_out = shift;
     for (int c = threadIdx.x * 8; c < ld_out; c += 256 * 8) {
         float v[8];
-        load_chunk(x + r * ld, c, cols, v);
+        load_chunk(x, c, cols, v);
         uint16_t h8[8], l8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
-            split(v[e] * s, h, l);
+            split(ldexpf(v[e], shift), h, l);
             h8[e] = bits(h);
             l8[e] = bits(l);
         }
-        *reinterpret_cast<uint4 *>(hi + r * ld_out + c) = *reinterpret_cast<const uint4 *>(h8);
-        *reinterpret_cast<uint4 *>(lo + r * ld_out + c) = *reinterpret_cast<const uint4 *>(l8);
+        *reinterpret_cast<uint4 *>(hi + c) = *reinterpret_cast<const uint4 *>(h8);
+        *reinterpret_cast<uint4 *>(lo + c) = *reinterpret_cast<const uint4 *>(l8);
     }
+}
+// x of the logits, with a scale for each row: none coarsens the others.
+__global__ __launch_bounds__(256) void k_planes_by_row(const float *x, int32_t cols, int64_t ld, int32_t *shift_out, uint16_t *hi, uint16_t *lo, int32_t ld_out) {
+    __shared__ float red[4];
+    const int64_t r = blockIdx.x;
+    const float most = block_max(largest_of_row(x + r * ld, cols), red);
+    row_as_planes(x + r * ld, cols, shift_for(exponent_of_most(most)), shift_out + r, hi + r * ld_out, lo + r * ld_out, ld_out);
+}
+
+// The backward pass's gain of each row, t * g_n, +0 for rows without an answer (whatever g_n holds there), and the exponent of the largest
+// finite magnitude of gain times x.  float32: x's rows that have a gain as planes, under a scale for each (see k_planes_by_row).
+template <typename T>
+__global__ __launch_bounds__(256) void k_gain(const Answers a, const float *row_grad, float t, const T *x, int64_t rows, int32_t cols, int64_t ld, float *gain, float *parts, int32_t *shift_out,
+                                              uint16_t *hi, uint16_t *lo, int32_t ld_out) {
+    __shared__ float red[4];
+    float most = kNoExponent;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        bool mine = false;
+        for (int k = threadIdx.x; k < a.top; k += 256) {
+            const int32_t i = a.idx[r * a.top + k];
+            mine |= i >= 0 && i < a.vocab;
+        }
+        const bool any = __syncthreads_or(mine);
+        const float g = any ? t * row_grad[r] : 0.0f;
+        if (threadIdx.x == 0) gain[r] = g;
+        if (g == 0.0f) continue;
+        float most_x = exponent_of_most(block_max(largest_of_row(x + r * ld, cols), red));
+        if (sizeof(T) == 4) row_as_planes(x + r * ld, cols, shift_for(most_x), shift_out + r, hi + r * ld_out, lo + r * ld_out, ld_out);
+        if (most_x > kNoExponent) most = fmaxf(most, most_x + static_cast<float>(exponent_of(g)));
+    }
+    if (threadIdx.x == 0) parts[blockIdx.x] = most;
 }
 
 // Three bfloat16 planes whose sum is v.
@@ -427,7 +435,7 @@ struct Picked {
     int32_t first;                     // vocabulary row that the piece begins with
 };
 struct StatsArgs {
-    const float *scale_x, *scale_w;    // NULL: 1
+    const int32_t *shift_x, *shift_w;  // of scaled planes, by row and of the piece; NULL: none
     float inv_t;
     float2 *stats;                     // [n][strips]: maximum, sum of exponentials around it
     int32_t strips, first_strip;       // strip of the piece's first row
@@ -441,11 +449,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_stats(const Problem p, const
     typename S::Sums acc;
     product<S>(p, tm, tn, part, (lds_char *)lds, acc);
     const Place<S> at(tm, tn);
-    const float piece = e.inv_t * (e.scale_w ? 1.0f / *e.scale_w : 1.0f);
+    const int shift_w = e.shift_w ? *e.shift_w : 0;
 #pragma unroll
     for (int j = 0; j < S::NI; ++j) {
         const int n = at.col(j);
-        const float unit = n < p.n && e.scale_x ? piece / e.scale_x[n] : piece;
+        const float unit = ldexpf(e.inv_t, -shift_w - (n < p.n && e.shift_x ? e.shift_x[n] : 0));
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
@@ -573,8 +581,8 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_loss(const T *x, i
 // C[n][v]: d as planes.  PAIRED: two neighbouring columns a lane, so that a store takes 4 bytes.  A piece of
 // d takes kPieceBytes at most (two passes of 131072 x 4096 x 8192: 38.9 ms with 128 MB, 35.9 with 256, 35.2 with 512).
 struct GradArgs {
-    const float *scales;               // many rows: kScaleX, kScaleW (both used where planes are), kScaleD; few rows: NULL
-    int planes_in;                     // the logits come from scaled planes
+    int many;                          // many rows: d has the gain's fraction alone (gain_in_d)
+    const int32_t *shift_x, *shift_w;  // of scaled planes that the logits come from, by row and of the piece; NULL: none
     float inv_t;
     const float *lse;
     Gains gains;
@@ -604,21 +612,21 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_grad(const Problem p, const 
     typename S::Sums acc;
     product<S>(p, tm, tn, part, (lds_char *)lds, acc);
     const Place<S> at(tm, tn);
-    // one scale after the other: their product may leave float32's range
-    const float unit = (e.planes_in ? e.inv_t / e.scales[kScaleX] / e.scales[kScaleW] : e.inv_t) * kLog2e;
-    const float scale_d = e.scales ? e.scales[kScaleD] : 1.0f;
+    const int shift_w = e.shift_w ? *e.shift_w : 0;
     __syncthreads();                               // the last stage has been read
-    float *row_lse = reinterpret_cast<float *>(lds), *row_gain = row_lse + S::TM;
-    int *row_target = reinterpret_cast<int *>(row_gain + S::TM);
+    float *row_lse = reinterpret_cast<float *>(lds), *row_gain = row_lse + S::TM, *row_unit = row_gain + S::TM;
+    int *row_target = reinterpret_cast<int *>(row_unit + S::TM);
     for (int i = threadIdx.x; i < S::TM; i += S::kThreads) {
         const int n = tm * S::TM + i;
         row_lse[i] = n < p.m ? e.lse[n] * kLog2e : 0.0f;
-        row_gain[i] = n < p.m ? e.gains.of(n) * scale_d : 0.0f;
+        const float gain = n < p.m ? e.gains.of(n) : 0.0f;
+        row_gain[i] = e.many ? gain_in_d(gain) : gain;
+        row_unit[i] = ldexpf(e.inv_t * kLog2e, -shift_w - (n < p.m && e.shift_x ? e.shift_x[n] : 0));
         if (ANSWER == kTarget) row_target[i] = n < p.m && e.answers.idx[n] >= e.first ? e.answers.idx[n] - e.first : -1;
     }
     float *spread = reinterpret_cast<float *>(row_target + S::TM);        // [TM][TN]: q
     if constexpr (ANSWER == kSpread) {
-        static_assert((3 * S::TM + S::TM * S::TN) * 4 <= S::kLds, "room for the tile");
+        static_assert((4 * S::TM + S::TM * S::TN) * 4 <= S::kLds, "room for the tile");
         for (int i = threadIdx.x; i < S::TM * S::TN; i += S::kThreads) spread[i] = 0.0f;
         __syncthreads();
         const int64_t begin = static_cast<int64_t>(tm) * S::TM * e.answers.top;
@@ -636,7 +644,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_grad(const Problem p, const 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int row = at.row(i, r) - tm * S::TM;
-            const float lse = row_lse[row], gain = row_gain[row];
+            const float lse = row_lse[row], gain = row_gain[row], unit = row_unit[row];
             const int target = ANSWER == kTarget ? row_target[row] : -1;
 #pragma unroll
             for (int j = 0; j < S::NI; j += kCols) {
@@ -668,7 +676,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_grad(const Problem p, const 
 
 // The answer's part of d for the piece of the vocabulary from `first` on: entries of a row name different tokens.
 template <int PLANES>
-__global__ __launch_bounds__(256) void k_subtract(const Answers a, const float *gain, const float *scales, int64_t rows, int32_t first, int32_t count, uint16_t *d, int64_t plane, int32_t ld) {
+__global__ __launch_bounds__(256) void k_subtract(const Answers a, const float *gain, int many, int64_t rows, int32_t first, int32_t count, uint16_t *d, int64_t plane, int32_t ld) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (i >= rows * a.top) return;
     const int64_t n = i / a.top;
@@ -680,7 +688,7 @@ __global__ __launch_bounds__(256) void k_subtract(const Answers a, const float *
 #pragma unroll
     for (int u = PLANES - 1; u >= 0; --u)
         prob += PLANES == 3 ? to_float(__builtin_bit_cast(bf16, to[u * plane])) : static_cast<float>(__builtin_bit_cast(_Float16, to[u * plane]));
-    planes_of<PLANES>(prob - a.q[i] * (gain[n] * (scales ? scales[kScaleD] : 1.0f)), p);
+    planes_of<PLANES>(prob - a.q[i] * (many ? gain_in_d(gain[n]) : gain[n]), p);
 #pragma unroll
     for (int u = 0; u < PLANES; ++u) to[u * plane] = p[u];
 }
@@ -688,9 +696,8 @@ __global__ __launch_bounds__(256) void k_subtract(const Answers a, const float *
 // dx: C[n][h] over the piece's vocabulary, added up over pieces in float32.  Where the tiles leave CUs without work the vocabulary is
 // cut into shares, whose sums k_input_grad_sum adds up in a fixed order (no atomics: the same inputs give the same bits).
 struct InputGradArgs {
-    const float *scales;               // NULL: 1
+    const int32_t *shift_w;            // many rows: d has the gain's fraction alone, W comes as scaled planes; NULL: neither
     Gains gains;
-    int planes_in;                     // W comes as a scaled plane
     int first, last;                   // piece
     float *sum;                        // [split][n][hidden]
     void *dx;
@@ -704,11 +711,16 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_input_grad(const Problem p, 
     typename S::Sums acc;
     product<S>(p, tm, tn, part, (lds_char *)lds, acc);
     const Place<S> at(tm, tn);
-    const float by_d = e.scales ? 1.0f / e.scales[kScaleD] : 1.0f, by_w = e.planes_in ? 1.0f / e.scales[kScaleW] : 1.0f;
     const bool whole = p.splits == 1;
     __syncthreads();                               // the last stage has been read
     float *row_on = reinterpret_cast<float *>(lds);
-    for (int i = threadIdx.x; i < S::TM; i += S::kThreads) row_on[i] = tm * S::TM + i < p.m && e.gains.of(tm * S::TM + i) != 0.0f ? 1.0f : 0.0f;
+    int *row_shift = reinterpret_cast<int *>(row_on + S::TM);
+    const int shift_w = e.shift_w ? *e.shift_w : 0;
+    for (int i = threadIdx.x; i < S::TM; i += S::kThreads) {
+        const float gain = tm * S::TM + i < p.m ? e.gains.of(tm * S::TM + i) : 0.0f;
+        row_on[i] = gain != 0.0f ? 1.0f : 0.0f;
+        row_shift[i] = e.shift_w ? exponent_of(gain) - kTop - shift_w : 0;
+    }
     __syncthreads();
     // the shares lie behind the sum over pieces
     const Window sum(e.sum + (whole ? 0 : (1 + static_cast<int64_t>(part)) * p.m * p.n), tm * S::TM, p.m, p.n, 4);
@@ -722,7 +734,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_input_grad(const Problem p, 
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const uint32_t row = at.row(i, r) - tm * S::TM, to = in ? (row * p.n + h) * 4u : kOutside;
-                float v = acc[i][j][r] * by_d * by_w;
+                float v = ldexpf(acc[i][j][r], row_shift[row]);
                 if (whole && !e.first) v += sum.get(to);
                 if (whole && e.last) dx.put(in ? (row * static_cast<uint32_t>(e.lddx) + h) * static_cast<uint32_t>(sizeof(T)) : kOutside, static_cast<T>(row_on[row] != 0.0f ? v : 0.0f));
                 else sum.put(to, v);
@@ -755,7 +767,7 @@ __global__ __launch_bounds__(256) void k_input_grad_sum(const InputGradArgs e, i
 
 // dW: C[v][h] over the rows, into the caller's float32 rows.
 struct WeightGradArgs {
-    const float *scales;               // NULL: 1
+    const int32_t *shift_x;            // many rows: x's scale, d's being kTop; NULL: neither has one
     float *dw;                         // of the piece's first row
     int accumulate;
 };
@@ -767,7 +779,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_weight_grad(const Problem p,
     typename S::Sums acc;
     product<S>(p, tm, tn, part, (lds_char *)lds, acc);
     const Place<S> at(tm, tn);
-    const float by_d = e.scales ? 1.0f / e.scales[kScaleD] : 1.0f, by_x = e.scales ? 1.0f / e.scales[kScaleX] : 1.0f;
+    const int shift = e.shift_x ? -kTop - *e.shift_x : 0;
     const Window dw(e.dw, tm * S::TM, p.m, p.n, 4);
 #pragma unroll
     for (int j = 0; j < S::NI; ++j) {
@@ -778,7 +790,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_weight_grad(const Problem p,
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const uint32_t to = in ? (static_cast<uint32_t>(at.row(i, r) - tm * S::TM) * p.n + h) * 4u : kOutside;
-                const float d = acc[i][j][r] * by_d * by_x;
+                const float d = ldexpf(acc[i][j][r], shift);
                 dw.put(to, e.accumulate ? dw.get(to) + d : d);
             }
     }
@@ -1541,7 +1553,7 @@ struct Layout {
     int32_t share;                     // direct: vocabulary rows of a share of dx
     int64_t x_plane, w_plane, d_plane; // elements from one plane to the next
     // offsets in the workspace
-    size_t idx, q, stats, gain, scales, parts_x, parts_w, scale_rows, x, x_raw, w, d, sum, total;
+    size_t idx, q, stats, gain, shifts, parts_x, parts_w, shift_rows, x, x_raw, w, d, sum, total;
 };
 
 // Whether dx of few rows takes the wide tile.  Both passes over 32768 rows of W, us, wide / 64 x 64: 40 tokens 4096 wide 334 / 349,
@@ -1580,17 +1592,17 @@ Layout layout_of(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, int
     }
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += static_cast<size_t>(up(bytes, 256)); return here; };
-    l.scales = take(kScales * 4);
-    l.parts_x = take(kMaxParts * 2 * 4);
+    l.shifts = take(kShifts * 4);
+    l.parts_x = take(kMaxParts * 4);
     l.parts_w = take(kMaxParts * 4);
     if (top > 0) {
         l.idx = take(rows * top * 4);
         l.q = take(rows * top * 4);
     }
     l.gain = take(rows * 4);
+    l.shift_rows = take(l.rows * 4);
     if (!backward) {
         l.stats = take(l.rows * l.strips * 8);
-        l.scale_rows = take(l.rows * 4);
     } else {
         l.d_plane = l.rows * d_cols;
         l.d = take(d_planes * l.d_plane * 2);
@@ -1607,7 +1619,8 @@ Layout layout_of(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, int
     }
     l.x_plane = up(l.rows * l.ld, 128);
     l.x = take((wide ? (l.few ? 3 : 2) : 1) * l.x_plane * 2);
-    if (!wide) l.x_raw = take(l.x_plane * 2);      // bfloat16 rows that cannot be read as they are
+    // x for the logits apart from x for dW: bfloat16 rows that cannot be read as they are; float32 planes by row
+    if (!wide || (backward && !l.few)) l.x_raw = take((wide ? 2 : 1) * l.x_plane * 2);
     l.w_plane = up(w_rows * l.ld, 128);
     l.w = take(w_planes * l.w_plane * 2);
     l.total = std::max<size_t>(256, at);
@@ -1689,11 +1702,11 @@ template <typename T>
 void lay_many(const Call &c, const Layout &l, const T *w, int64_t count, uint16_t *hi, uint16_t *lo) {
     const int64_t chunks = count * l.ld / 8;
     const unsigned g = blocks_for((chunks + 255) / 256, kMaxParts), more = blocks_for((chunks + 255) / 256, kPlaneBlocks);
-    float *parts = in_ws<float>(c, l.parts_w), *scale = in_ws<float>(c, l.scales) + kScaleW, *none = nullptr;
+    float *parts = in_ws<float>(c, l.parts_w);
     const int cols = static_cast<int>(c.hidden), ld = static_cast<int>(l.ld);
     const float *every_row = nullptr;
     hipLaunchKernelGGL((k_largest<T>), dim3(g), dim3(256), 0, c.stream, w, count, cols, c.ldw, parts);
-    hipLaunchKernelGGL((k_planes<T>), dim3(more), dim3(256), 0, c.stream, w, count, cols, c.ldw, every_row, parts, static_cast<int>(g), scale, none, hi, lo, ld);
+    hipLaunchKernelGGL((k_planes<T>), dim3(more), dim3(256), 0, c.stream, w, count, cols, c.ldw, every_row, parts, static_cast<int>(g), in_ws<int32_t>(c, l.shifts) + kShiftW, hi, lo, ld);
 }
 void align_rows(const Call &c, const Layout &l, const void *x, int64_t rows, int64_t ld, uint16_t *out) {
     hipLaunchKernelGGL(k_align, dim3(blocks_for(rows, kPlaneBlocks)), dim3(256), 0, c.stream, static_cast<const bf16 *>(x), rows, static_cast<int>(c.hidden), ld, out,
@@ -1715,7 +1728,7 @@ void launch_stats(const Call &c, const Layout &l, int64_t first_row, int64_t row
     uint16_t *xs = in_ws<uint16_t>(c, l.x), *ws = in_ws<uint16_t>(c, l.w);
     if (wide)
         hipLaunchKernelGGL(k_planes_by_row, dim3(static_cast<unsigned>(rows)), dim3(256), 0, c.stream, reinterpret_cast<const float *>(x), static_cast<int>(c.hidden), c.ldx,
-                           in_ws<float>(c, l.scale_rows), xs, xs + l.x_plane, static_cast<int>(l.ld));
+                           in_ws<int32_t>(c, l.shift_rows), xs, xs + l.x_plane, static_cast<int>(l.ld));
     else if (!x_as_is) align_rows(c, l, x, rows, c.ldx, xs);
     const Operand xo = x_as_is ? operand(x, c.ldx, 0) : operand(xs, l.ld, l.x_plane);
     for (int64_t first = 0; first < c.vocab; first += l.piece) {
@@ -1725,7 +1738,7 @@ void launch_stats(const Call &c, const Layout &l, int64_t first_row, int64_t row
         else if (!w_as_is) align_rows(c, l, w, count, c.ldw, ws);
         const Operand wo = w_as_is ? operand(w, c.ldw, 0) : operand(ws, l.ld, l.w_plane);
         Problem p = problem(wo, xo, count, rows, c.hidden);
-        const StatsArgs e = {wide ? in_ws<float>(c, l.scale_rows) : nullptr, wide ? in_ws<float>(c, l.scales) + kScaleW : nullptr, 1.0f / c.t, in_ws<float2>(c, l.stats), l.strips,
+        const StatsArgs e = {wide ? in_ws<int32_t>(c, l.shift_rows) : nullptr, wide ? in_ws<int32_t>(c, l.shifts) + kShiftW : nullptr, 1.0f / c.t, in_ws<float2>(c, l.stats), l.strips,
                              static_cast<int32_t>(first / kStripOf[l.stats_tile]), picked_by(c, l, first_row, first)};
         with_shape<V, false, false, false, PLANES, PLANES>(l.stats_tile, [&](auto shape) {
             using S = decltype(shape);
@@ -1757,12 +1770,12 @@ void launch_loss(const Call &c, const Layout &l, int64_t first_row, int64_t rows
 template <class S, int PLANES>
 void launch_grad(const Call &c, Problem &p, const GradArgs &e, const float *gain) {
     const dim3 grid = cut<S>(p, 1), threads(S::kThreads);
-    constexpr Answer kSeveral = (3 * S::TM + S::TM * S::TN) * 4 <= S::kLds ? kSpread : kLater;
+    constexpr Answer kSeveral = (4 * S::TM + S::TM * S::TN) * 4 <= S::kLds ? kSpread : kLater;
     if (!c.top) hipLaunchKernelGGL((k_grad<S, PLANES, kTarget>), grid, threads, 0, c.stream, p, e);
     else hipLaunchKernelGGL((k_grad<S, PLANES, kSeveral>), grid, threads, 0, c.stream, p, e);
     if (c.top && kSeveral == kLater)
         hipLaunchKernelGGL((k_subtract<PLANES>), dim3(static_cast<unsigned>((static_cast<int64_t>(p.m) * e.answers.top + 255) / 256)), dim3(256), 0, c.stream, e.answers, gain,
-                           e.scales, static_cast<int64_t>(p.m), e.first, p.n, e.d, e.plane, e.ld);
+                           e.many, static_cast<int64_t>(p.m), e.first, p.n, e.d, e.plane, e.ld);
 }
 
 template <typename T>
@@ -1877,20 +1890,20 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
     const bool wide = c.dtype == RSDGC_F32, few = l.few, x_as_is = takes_as_is(c.dtype, c.x, c.ldx, c.hidden), w_as_is = takes_as_is(c.dtype, c.w, c.ldw, c.hidden);
     const int cols = static_cast<int>(c.hidden), ld = static_cast<int>(l.ld);
     const T *x = static_cast<const T *>(c.x) + first_row * c.ldx;
-    float *scales = few ? nullptr : in_ws<float>(c, l.scales), *parts = in_ws<float>(c, l.parts_x), *gain = in_ws<float>(c, l.gain) + first_row;
+    float *parts = in_ws<float>(c, l.parts_x), *gain = in_ws<float>(c, l.gain) + first_row;
+    int32_t *shifts = in_ws<int32_t>(c, l.shifts), *shift_rows = in_ws<int32_t>(c, l.shift_rows);
     uint16_t *xs = in_ws<uint16_t>(c, l.x), *x_raw = in_ws<uint16_t>(c, l.x_raw), *ws = in_ws<uint16_t>(c, l.w), *d = in_ws<uint16_t>(c, l.d);
     const Answers a = answers_of(c, l, first_row);
     const Gains gains = few && !c.top ? Gains{nullptr, c.row_grad + first_row, a.idx, a.vocab} : Gains{gain, nullptr, nullptr, 0};
     if (!few) {
         const unsigned g = blocks_for(rows, kMaxParts), more = blocks_for((rows * l.ld / 8 + 255) / 256, kPlaneBlocks);
         uint16_t *second = wide ? xs + l.x_plane : nullptr;
-        hipLaunchKernelGGL((k_gain<T>), dim3(g), dim3(256), 0, c.stream, a, c.row_grad + first_row, c.t, x, rows, cols, c.ldx, gain, parts);
-        hipLaunchKernelGGL((k_planes<T>), dim3(more), dim3(256), 0, c.stream, x, rows, cols, c.ldx, gain, parts, static_cast<int>(g), scales + kScaleX,
-                           scales + kScaleD, xs, second, ld);
+        hipLaunchKernelGGL((k_gain<T>), dim3(g), dim3(256), 0, c.stream, a, c.row_grad + first_row, c.t, x, rows, cols, c.ldx, gain, parts, shift_rows, x_raw, x_raw + l.x_plane, ld);
+        hipLaunchKernelGGL((k_planes<T>), dim3(more), dim3(256), 0, c.stream, x, rows, cols, c.ldx, gain, parts, static_cast<int>(g), shifts + kShiftX, xs, second, ld);
         if (!wide && !x_as_is) align_rows(c, l, x, rows, c.ldx, x_raw);
     }
-    // for the logits: as it is, its planes (float32; few rows: the copy without the rows that have no answer), or the copy
-    const Operand xo = x_as_is ? operand(x, c.ldx, 0) : wide || few ? operand(xs, l.ld, l.x_plane) : operand(x_raw, l.ld, 0);
+    // for the logits: as it is, planes under a scale by row (float32), or the copy (few rows: without the rows that have no answer)
+    const Operand xo = x_as_is ? operand(x, c.ldx, 0) : few ? operand(xs, l.ld, l.x_plane) : operand(x_raw, l.ld, l.x_plane);
     const Operand x_planes = operand(xs, l.ld, l.x_plane);
     for (int64_t first = 0; first < c.vocab; first += l.piece) {
         const int64_t count = std::min(l.piece, c.vocab - first);
@@ -1905,11 +1918,11 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
         if (l.direct) launch_few_grad<T>(c, l, first, count, gains, a);
         else if constexpr (PLANES < 3) {
             Problem p = problem(xo, wo, rows, count, c.hidden);
-            const GradArgs e = {scales, wide && !few, 1.0f / c.t, c.lse + first_row, gains, a, static_cast<int32_t>(first), d, l.d_plane, ldd};
+            const GradArgs e = {!few, wide ? shift_rows : nullptr, wide ? shifts + kShiftW : nullptr, 1.0f / c.t, c.lse + first_row, gains, a, static_cast<int32_t>(first), d, l.d_plane, ldd};
             with_shape<V, false, false, true, PLANES, PLANES>(choose(rows, count, c.hidden, 1).tile,
                                                               [&](auto shape) { launch_grad<decltype(shape), D_PLANES>(c, p, e, gain); });
         }
-        const InputGradArgs dx = {scales, gains, !few, first == 0, first + count == c.vocab, in_ws<float>(c, l.sum), static_cast<T *>(c.dx) + first_row * c.lddx, c.lddx};
+        const InputGradArgs dx = {few ? nullptr : shifts + kShiftW, gains, first == 0, first + count == c.vocab, in_ws<float>(c, l.sum), static_cast<T *>(c.dx) + first_row * c.lddx, c.lddx};
         if (l.direct) launch_few_input<T>(c, l, first, count, dx);
         else if constexpr (PLANES < 3) {
             Operand wd = wo;
@@ -1934,7 +1947,7 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
             launch_few_weight<T>(c, d_planes, count, {x, c.ldx, gains, c.dw + first * c.hidden, accumulate, 0});
         } else {
             Problem p = problem(d_planes, x_planes, count, c.hidden, rows);
-            const WeightGradArgs e = {scales, c.dw + first * c.hidden, accumulate};
+            const WeightGradArgs e = {few ? nullptr : shifts + kShiftX, c.dw + first * c.hidden, accumulate};
             with_shape<D, true, true, false, D_PLANES, PLANES>(choose(count, c.hidden, rows, 1, D_PLANES == 3 ? kTile64 : kTile256).tile, [&](auto shape) {
                 using S = decltype(shape);
                 const dim3 grid = cut<S>(p, 1);

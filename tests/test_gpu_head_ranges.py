@@ -208,3 +208,46 @@ def test_words_that_are_much_alike(dtype, rows, hidden, vocab, top):
     case["w"].copy_(shared + 0.01 * torch.randn(vocab, hidden, generator=gen, device="cuda"))
     case["x"].copy_(torch.randn(rows, hidden, generator=gen, device="cuda"))
     _check(f"alike {rows}x{hidden}x{vocab} top {top} {dtype}", case, 2.0 if top else 1.0)
+
+
+def _check_rows(tag, case, t=1.0, but=None):
+    """Every token's loss, lse and dx against its own size, not that of the largest, and dw as a whole; but one token's, and dw then not."""
+    print("head", tag, flush=True)
+    got, (want, terms) = _head_run(case, t), _exact(case, t)
+    kind = case["x"].dtype
+    keep = torch.arange(case["x"].shape[0], device="cuda") != (-1 if but is None else but)
+    for k in ("loss", "lse"):
+        off, size = (got[k].double() - want[k]).abs()[keep], (want["lse"].abs() + want["loss"].abs())[keep]
+        assert float((off / size).max()) <= 1e-5, (tag, k, float((off / size).max()))
+    off = (got["dx"].double() - want["dx"]).norm(dim=1)
+    may = {F32: 1e-5, BF16: 3e-3}[kind] * want["dx"].norm(dim=1) + 1e-5 * terms["dx"].norm(dim=1)
+    worst = int(torch.where(keep, off - may, -math.inf).argmax())
+    assert bool((off <= may)[keep].all()), f"{tag}: row {worst} of dx is {float(off[worst] / want['dx'][worst].norm()):.3g} off"
+    if but is None:
+        _close(f"{tag} dw", got["dw"], want["dw"].cpu(), F32, terms["dw"].cpu())
+
+
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,hidden", [(20, 64), (700, 64), (700, 61), (16384 + 40, 24)])
+def test_tokens_whose_gradients_differ_by_many_orders(rows, hidden, dtype, top):
+    """row_grad from 1e-28 to 1: a token's row of dx does not know the others' gradients."""
+    case = _case(rows, hidden, 300, dtype, top, seed=rows)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    case["row_grad"] = torch.pow(10.0, -28 * torch.rand(rows, generator=gen, device="cuda")) * (1 - 2 * (torch.rand(rows, generator=gen, device="cuda") < 0.3))
+    _check_rows(f"gains {rows}x{hidden} top {top} {dtype}", case, 2.0 if top else 1.0)
+
+
+@pytest.mark.parametrize("top", [0, 6])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("outlier", [1e4, 1e10])
+@pytest.mark.parametrize("rows", [20, 700])
+def test_a_token_with_a_channel_far_above_the_others(rows, outlier, dtype, top):
+    """One token's channel that the matrix does not read: the other tokens' logits, losses and dx do not know of it."""
+    case = _case(rows, 64, 300, dtype, top, seed=rows)
+    case["w"][:, 0] = 0
+    case["x"][5, 0] = outlier
+    for k in ("target", "top_idx"):
+        if k in case:
+            case[k][5] = 7
+    _check_rows(f"outlier {outlier} in {rows} top {top} {dtype}", case, 2.0 if top else 1.0, but=5)

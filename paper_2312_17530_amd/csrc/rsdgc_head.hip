@@ -73,10 +73,6 @@ int64_t few_rows(int32_t dtype, bool as_is, bool backward) {
     const bool unaligned = dtype == RSDGC_BF16 && !as_is;
     return backward ? (unaligned ? 256 : 160) : unaligned ? 1024 : 384;
 }
-// Up to so many rows a teacher's answers are formed by the workgroup that takes the row's loss, not in a launch before.  Loss of 64
-// logits a row, 16384 x 1024, us, inside / before: 16 rows 20 / 37, 128 rows 23 / 41, 384 rows 40 / 50, 768 rows 60 / 62, 1500 rows 115 / 112.
-constexpr int64_t kFewAnswers = 768;
-
 // ------------------------------------------------------------------ answers
 // A token's answer: `top` entries idx / q (q NULL: ones), an entry counts where 0 <= idx < vocab.
 struct Answers {
@@ -135,13 +131,13 @@ __device__ __forceinline__ bool row_answers(const Teacher &a, int64_t row, int32
     }
     return sum > 0.0f;
 }
-// The same for all rows, a wave each, and (gain not NULL) the backward pass's gain: t * g_n, +0 for a row without an answer.
+// The same for all rows, a wave each, and the backward pass's gain: t * g_n, +0 for a row without an answer.
 __global__ __launch_bounds__(256) void k_answers(const Teacher a, int64_t rows, int32_t *idx, float *q, const float *row_grad, float t, float *gain) {
     extern __shared__ int32_t lds_answers[];       // [4][2][top]
     const int wave = threadIdx.x >> 6;
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave; row < rows; row += static_cast<int64_t>(gridDim.x) * 4) {
         const bool any = row_answers(a, row, lds_answers + wave * 2 * a.top, idx + row * a.top, q + row * a.top);
-        if (gain && (threadIdx.x & 63) == 0) gain[row] = any ? t * row_grad[row] : 0.0f;
+        if ((threadIdx.x & 63) == 0) gain[row] = any ? t * row_grad[row] : 0.0f;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // the room has been read
     }
 }
@@ -429,11 +425,34 @@ __global__ __launch_bounds__(256) void k_clear(float *p, int64_t n) {
 // formed in registers and one exchange between the wave's halves; 8 bytes for each token and strip are all that is written.
 // One target a row: its logit, which is left out of the strips, so that the loss of a token that is nearly sure of its answer, the
 // logarithm of 1 + little, is as good as the little.
+// A teacher's entries: their logits, of the same sums as the strips', so that what is wrong with them cancels in a small loss.
 struct Picked {
     const int32_t *target;             // one token a row, or NULL
-    float *logit;                      // [n]
+    const int32_t *entries;            // ... or `top` of them
+    int32_t top;
+    float *logit;                      // [n][max(1, top)]
     int32_t first;                     // vocabulary row that the piece begins with
 };
+// The logits of those entries of tokens n0 .. n0 + count that name one of `rows` vocabulary rows from `from` on; at(token, row) is in LDS.
+template <int THREADS, typename F>
+__device__ __forceinline__ void pick(const Picked &p, int n0, int count, int from, int rows, const F &at) {
+    const int32_t *entries = p.entries + static_cast<int64_t>(n0) * p.top;
+    float *logit = p.logit + static_cast<int64_t>(n0) * p.top;
+    const int all = count * p.top;
+#pragma unroll 4
+    for (int i = 4 * threadIdx.x; i < all; i += 4 * THREADS) {
+        int32_t four[4] = {-1, -1, -1, -1};
+        if (i + 4 <= all) __builtin_memcpy(four, entries + i, sizeof(four));
+        else
+#pragma unroll
+            for (int u = 0; u < 4; ++u) four[u] = i + u < all ? entries[i + u] : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t v = static_cast<uint32_t>(four[u]) - static_cast<uint32_t>(from);     // negative entries: beyond
+            if (v < static_cast<uint32_t>(rows)) logit[i + u] = at((i + u) / p.top, static_cast<int>(v));
+        }
+    }
+}
 struct StatsArgs {
     const int32_t *shift_x, *shift_w;  // of scaled planes, by row and of the piece; NULL: none
     float inv_t;
@@ -490,19 +509,38 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_stats(const Problem p, const
         sum += __shfl_xor(sum, 32);
         if (at.lane < 32 && n < p.n && at.row0 < p.m) e.stats[static_cast<int64_t>(n) * e.strips + e.first_strip + at.row0 / (S::MI * 32)] = make_float2(most, sum);
     }
+    if (!e.picked.entries) return;
+    // the tile's logits through LDS, those of one strip after the other: [token][row]
+    constexpr int kDown = S::MI * 32, kLine = kDown + 4;
+    static_assert(S::TN * kLine * 4 <= S::kLds, "room for a strip");
+    float *tile = reinterpret_cast<float *>(lds);
+    for (int strip = 0; strip < S::WM; ++strip) {
+        __syncthreads();                           // the last stage, or the strip before, has been read
+        if (static_cast<int>(threadIdx.x >> 6) / S::WN == strip)
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *reinterpret_cast<float4 *>(tile + (at.col(j) - tn * S::TN) * kLine + 32 * i + 2 * r + 4 * (at.lane >> 5)) =
+                            make_float4(acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]);
+        __syncthreads();
+        const int v0 = tm * S::TM + strip * kDown;
+        pick<S::kThreads>(e.picked, tn * S::TN, min(S::TN, p.n - tn * S::TN), e.picked.first + v0, max(0, min(kDown, p.m - v0)),
+                          [&](int n, int v) { return tile[n * kLine + v]; });
+    }
 }
 
-// lse from a token's strips, and the loss.  5 to 14 us for a target; behind a teacher 4096 rows of 64 entries, 2048 wide, take 162 us
-// = 6.6 TB/s of W's rows, most of them from the caches.  WAVES waves per row.  1: the answer is one target (see Picked).  More: a teacher's, whose
-// logits are dot products; 4: laid down before (answers), 16, few rows: formed here first.
-template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_loss(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t rows, int32_t hidden, const float2 *stats, int32_t strips,
-                                              const int32_t *target, const float *picked, int32_t vocab, const Answers answers, const Teacher teacher, float t, float *loss, float *lse_out) {
-    extern __shared__ int32_t lds_answers[];       // [4][top]: idx, q, and room
-    __shared__ float part[16];
+// lse from a token's strips, and the loss, a wave for each token.  picked: the logits of its one target (see Picked), or of a teacher's
+// entries, whose shares are formed here.
+template <bool TAUGHT>
+__global__ __launch_bounds__(256) void k_loss(int64_t rows, const float2 *stats, int32_t strips, const int32_t *target, const float *picked, int32_t vocab, const Teacher teacher, float t,
+                                              float *loss, float *lse_out) {
+    extern __shared__ int32_t lds_answers[];       // [4][4][top]: idx, q, and room
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
-    if (WAVES == 1 && row >= rows) return;         // with WAVES > 1 the grid holds no other rows
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    if (row >= rows) return;
     const float2 *s = stats + row * strips;
     // a running maximum and sum, eight strips at a time
     float most = -INFINITY, sum = 0.0f;
@@ -522,7 +560,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_loss(const T *x, i
     const float all = wave_max(most), around = all > -INFINITY ? all : 0.0f;
     sum *= exp2f((most - around) * kLog2e);
     sum = wave_sum(sum);
-    if constexpr (WAVES == 1) {
+    if constexpr (!TAUGHT) {
         const int32_t i = target[row];
         if (lane) return;
         if (i < 0 || i >= vocab) {
@@ -536,45 +574,18 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_loss(const T *x, i
         }
         return;
     }
-    const float log_sum = logf(sum), lse = around + log_sum;
-    float l = 0.0f;
-    const T *u = x + row * ldx;
     const int top = teacher.top;
-    const int32_t *idx = answers.idx + row * top;
-    const float *qs = answers.q + row * top;
-    if (WAVES == 16) {
-        float *q = reinterpret_cast<float *>(lds_answers + top);
-        if (wave == 0) row_answers(teacher, row, lds_answers + 2 * top, lds_answers, q);
-        __syncthreads();
-        idx = lds_answers;
-        qs = q;
-    }
-    const int whole = hidden & ~7;                                // eight elements at a time, the rest one by one
-    for (int k = wave; k < top; k += WAVES) {
-        const int32_t i = idx[k];
-        if (i < 0 || i >= vocab) continue;
-        const T *v = w + static_cast<int64_t>(i) * ldw;
-        float dot = 0.0f;
-#pragma unroll 4
-        for (int c = lane * 8; c < whole; c += 512) {
-            T p[8], r[8];
-            __builtin_memcpy(p, u + c, sizeof(p));
-            __builtin_memcpy(r, v + c, sizeof(r));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot = fmaf(to_float(p[e]), to_float(r[e]), dot);
-        }
-        if (whole + lane < hidden) dot = fmaf(to_float(u[whole + lane]), to_float(v[whole + lane]), dot);
-        const float z = wave_sum(dot) / t, q = qs[k];
-        if (q > 0.0f) l += q * (logf(q) + ((around - z) + log_sum));
-    }
-    if (lane == 0) part[wave] = l;
-    __syncthreads();
-    l = 0.0f;
-    for (int u = 0; u < WAVES; ++u) l += part[u];
-    if (wave == 0 && lane == 0) {
-        loss[row] = t * (t * l);                   // the square may leave the range
-        lse_out[row] = lse;
-    }
+    int32_t *idx = lds_answers + wave * 4 * top;
+    float *q = reinterpret_cast<float *>(idx + top);
+    row_answers(teacher, row, idx + 2 * top, idx, q);
+    const float log_sum = logf(sum);
+    float l = 0.0f;
+    for (int k = lane; k < top; k += 64)                          // a lane's own entries
+        if (idx[k] >= 0 && q[k] > 0.0f) l += q[k] * (logf(q[k]) + ((around - picked[row * top + k]) + log_sum));
+    l = wave_sum(l);
+    if (lane) return;
+    loss[row] = t * (t * l);                       // the square may leave the range
+    lse_out[row] = around + log_sum;
 }
 
 // ----------------------------------------------------------------- backward
@@ -966,8 +977,9 @@ struct FewLogits {
     int64_t plane;
     int32_t ld;
 };
-// What becomes of the logits: a maximum and a sum (kStats), or d of an answer of one (kOne) or several tokens (kMore).
-enum Purpose { kStats, kOne, kMore };
+// What becomes of the logits: a maximum and a sum, and an answer's own logits, of one token (kStats) or several (kTaught), or d of an
+// answer of one (kOne) or several tokens (kMore).
+enum Purpose { kStats, kTaught, kOne, kMore };
 // k of a stage that a wave takes
 template <typename T, int NB, int WK> constexpr int kFewStage = (sizeof(T) == 4 && (NB > 1 || WK > 1) ? 32 : 64) / (WK == 1 ? 1 : 2);
 // p: C[v][n], b: x's planes.  A wave takes 32 vocabulary rows and NB * 32 tokens; WK of a workgroup's four waves share the k axis of
@@ -975,7 +987,7 @@ template <typename T, int NB, int WK> constexpr int kFewStage = (sizeof(T) == 4 
 template <typename T, int NB, int WK, Purpose FOR>
 __global__ __launch_bounds__(256, WK == 4 && NB == 4 ? 1 : 2) void k_few_logits(const Problem p, const FewLogits<T> e) {
     constexpr int P = kPlanesOf<T>, kMine = kFewStage<T, NB, WK>, KS = kMine * WK, kN = NB * 32, kM = 128 / WK, kPlane = kN * KS * 2, kStage = P * kPlane, kFrags = kMine / 16;
-    constexpr int kSpread = FOR == kMore ? kM * kN * 4 : 0, kLds = kSpread > 3 * kStage ? kSpread : 3 * kStage;
+    constexpr int kSpread = FOR == kMore || FOR == kTaught ? kM * kN * 4 : 0, kLds = kSpread > 3 * kStage ? kSpread : 3 * kStage;
     static_assert(WK == 1 || 2 * kN * 32 * 4 <= kLds, "room for two waves' sums");
     using Load = Loader<false, kN, 256, false, KS>;
     __shared__ __attribute__((aligned(16))) char lds_room[kLds];
@@ -1097,8 +1109,12 @@ __global__ __launch_bounds__(256, WK == 4 && NB == 4 ? 1 : 2) void k_few_logits(
         }
     }
     const bool last = WK == 1 || wave == 0;                          // holds the sums
-    if constexpr (FOR == kStats) {
-        if (v0 >= p.m || !last) return;
+    if constexpr (FOR == kStats || FOR == kTaught) {
+        const bool here = v0 < p.m && last;
+        if (FOR == kStats && !here) return;
+        float *tile = reinterpret_cast<float *>(lds_room);           // kTaught: [kM][kN], the logits
+        if (FOR == kTaught) __syncthreads();                         // the last stage has been read
+        if (here)
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int n = tn * kN + 32 * j + (lane & 31);
@@ -1108,7 +1124,10 @@ __global__ __launch_bounds__(256, WK == 4 && NB == 4 ? 1 : 2) void k_few_logits(
                 acc[j][r] = v0 + 8 * (r >> 2) + 4 * half + (r & 3) < p.m ? acc[j][r] * e.inv_t : -INFINITY;
                 most = fmaxf(most, acc[j][r]);
             }
-            if (e.picked.target) {
+            if (FOR == kTaught) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) tile[(v0 - tm * kM + 8 * (r >> 2) + 4 * half + (r & 3)) * kN + 32 * j + (lane & 31)] = acc[j][r];
+            } else {
                 const int32_t target = n < p.n ? e.picked.target[n] : -1, from = e.picked.first + v0;
                 if (target >= from && target < e.picked.first + min(p.m, v0 + 32)) {                // rare
                     const int own = target - from - 4 * half;        // one of the wave's halves has it
@@ -1130,6 +1149,10 @@ __global__ __launch_bounds__(256, WK == 4 && NB == 4 ? 1 : 2) void k_few_logits(
             for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[j][r] - around) * kLog2e);
             sum += __shfl_xor(sum, 32);
             if (half == 0 && n < p.n) e.stats[static_cast<int64_t>(n) * e.strips + e.first_strip + v0 / 32] = make_float2(most, sum);
+        }
+        if constexpr (FOR == kTaught) {
+            __syncthreads();
+            pick<256>(e.picked, tn * kN, min(kN, p.n - tn * kN), e.picked.first + tm * kM, max(0, min(kM, p.m - tm * kM)), [&](int n, int v) { return tile[v * kN + n]; });
         }
     } else {
         float *spread = reinterpret_cast<float *>(lds_room);         // [kM][kN]: q
@@ -1553,7 +1576,7 @@ struct Layout {
     int32_t share;                     // direct: vocabulary rows of a share of dx
     int64_t x_plane, w_plane, d_plane; // elements from one plane to the next
     // offsets in the workspace
-    size_t idx, q, stats, gain, shifts, parts_x, parts_w, shift_rows, x, x_raw, w, d, sum, total;
+    size_t idx, q, stats, picked, gain, shifts, parts_x, parts_w, shift_rows, x, x_raw, w, d, sum, total;
 };
 
 // Whether dx of few rows takes the wide tile.  Both passes over 32768 rows of W, us, wide / 64 x 64: 40 tokens 4096 wide 334 / 349,
@@ -1595,15 +1618,16 @@ Layout layout_of(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, int
     l.shifts = take(kShifts * 4);
     l.parts_x = take(kMaxParts * 4);
     l.parts_w = take(kMaxParts * 4);
-    if (top > 0) {
-        l.idx = take(rows * top * 4);
-        l.q = take(rows * top * 4);
-    }
-    l.gain = take(rows * 4);
     l.shift_rows = take(l.rows * 4);
     if (!backward) {
         l.stats = take(l.rows * l.strips * 8);
+        l.picked = take(l.rows * std::max<int64_t>(1, top) * 4);
     } else {
+        if (top > 0) {
+            l.idx = take(rows * top * 4);
+            l.q = take(rows * top * 4);
+        }
+        l.gain = take(rows * 4);
         l.d_plane = l.rows * d_cols;
         l.d = take(d_planes * l.d_plane * 2);
         // shares for at least 512 workgroups, as far as the tiles alone do not give them
@@ -1671,18 +1695,18 @@ Answers answers_of(const Call &c, const Layout &l, int64_t first_row) {
     }
     return a;
 }
-// The forward pass has no gains; their place takes the targets' logits.
 Picked picked_by(const Call &c, const Layout &l, int64_t first_row, int64_t first) {
-    return {c.top ? nullptr : c.idx + first_row, in_ws<float>(c, l.gain), static_cast<int32_t>(first)};
+    const bool one = c.top == 0;
+    return {one ? c.idx + first_row : nullptr, one ? nullptr : c.idx + first_row * c.top, c.top, in_ws<float>(c, l.picked), static_cast<int32_t>(first)};
 }
 Teacher teacher_of(const Call &c, int64_t first_row) {
     return {c.idx + first_row * c.top, c.logit + first_row * c.top, c.top, static_cast<int32_t>(c.vocab), 1.0f / c.t};
 }
 constexpr int64_t kAnswerBlocks = int64_t(1) << 20;      // a launch has less than 2^32 threads
 size_t answer_room(const Call &c) { return static_cast<size_t>(c.top) * 32; }      // LDS of four waves
-void launch_answers(const Call &c, const Layout &l, bool backward) {
+void launch_answers(const Call &c, const Layout &l) {
     hipLaunchKernelGGL(k_answers, dim3(blocks_for((c.rows + 3) / 4, kAnswerBlocks)), dim3(256), answer_room(c), c.stream, teacher_of(c, 0), c.rows, in_ws<int32_t>(c, l.idx),
-                       in_ws<float>(c, l.q), c.row_grad, c.t, backward ? in_ws<float>(c, l.gain) : static_cast<float *>(nullptr));
+                       in_ws<float>(c, l.q), c.row_grad, c.t, in_ws<float>(c, l.gain));
 }
 
 // Few rows: x's rows as bfloat16 planes.  gains: rows without an answer come out as zeros; behind a teacher its answers and the
@@ -1748,23 +1772,14 @@ void launch_stats(const Call &c, const Layout &l, int64_t first_row, int64_t row
     }
 }
 
-template <typename T>
 void launch_loss(const Call &c, const Layout &l, int64_t first_row, int64_t rows) {
-    const T *x = static_cast<const T *>(c.x) + first_row * c.ldx, *w = static_cast<const T *>(c.w);
-    const int hidden = static_cast<int>(c.hidden), vocab = static_cast<int>(c.vocab);
+    const int vocab = static_cast<int>(c.vocab);
+    const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
     const float2 *stats = in_ws<float2>(c, l.stats);
+    const float *picked = in_ws<float>(c, l.picked);
     float *loss = c.loss + first_row, *lse = c.lse_out + first_row;
-    const int32_t *target = c.idx + first_row;
-    const float *picked = in_ws<float>(c, l.gain);
-    if (!c.top)
-        hipLaunchKernelGGL((k_loss<T, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, c.stream, x, c.ldx, w, c.ldw, rows, hidden, stats, l.strips, target, picked, vocab,
-                           Answers{}, Teacher{}, c.t, loss, lse);
-    else if (c.rows <= kFewAnswers)
-        hipLaunchKernelGGL((k_loss<T, 16>), dim3(static_cast<unsigned>(rows)), dim3(1024), answer_room(c) / 2, c.stream, x, c.ldx, w, c.ldw, rows, hidden, stats, l.strips, target, picked, vocab,
-                           Answers{}, teacher_of(c, first_row), c.t, loss, lse);
-    else
-        hipLaunchKernelGGL((k_loss<T, 4>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, c.stream, x, c.ldx, w, c.ldw, rows, hidden, stats, l.strips, target, picked, vocab,
-                           answers_of(c, l, first_row), teacher_of(c, first_row), c.t, loss, lse);
+    if (c.top) hipLaunchKernelGGL((k_loss<true>), grid, dim3(256), 2 * answer_room(c), c.stream, rows, stats, l.strips, static_cast<const int32_t *>(nullptr), picked, vocab, teacher_of(c, first_row), c.t, loss, lse);
+    else hipLaunchKernelGGL((k_loss<false>), grid, dim3(256), 0, c.stream, rows, stats, l.strips, c.idx + first_row, picked, vocab, Teacher{}, c.t, loss, lse);
 }
 
 template <class S, int PLANES>
@@ -1832,7 +1847,8 @@ void launch_few_stats(const Call &c, const Layout &l) {
     e.stats = in_ws<float2>(c, l.stats);
     e.strips = l.strips;
     e.picked = picked_by(c, l, 0, 0);
-    launch_few_logits<T, kStats>(c, l, 0, c.vocab, e);
+    if (c.top) launch_few_logits<T, kTaught>(c, l, 0, c.vocab, e);
+    else launch_few_logits<T, kStats>(c, l, 0, c.vocab, e);
 }
 template <typename T>
 void launch_few_grad(const Call &c, const Layout &l, int64_t first, int64_t count, const Gains &gains, const Answers &answers) {
@@ -2001,18 +2017,16 @@ int forward(const Call &c, const char *what) {
     Range read[4];
     read_by(c, read);
     if (!apart(written, 3, read, 4)) return RSDGC_EINVAL;
-    if (c.top && c.rows > kFewAnswers) launch_answers(c, l, false);
     for (int64_t first = 0; first < c.rows; first += l.rows) {
         const int64_t rows = std::min(l.rows, c.rows - first);
         if (c.dtype == RSDGC_BF16) {
             if (l.direct) launch_few_stats<bf16>(c, l);
             else launch_stats<bf16, bfloat8, 1>(c, l, first, rows);
-            launch_loss<bf16>(c, l, first, rows);
         } else {
             if (l.direct) launch_few_stats<float>(c, l);
             else launch_stats<float, half8, 2>(c, l, first, rows);
-            launch_loss<float>(c, l, first, rows);
         }
+        launch_loss(c, l, first, rows);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? RSDGC_OK : remember_hip_error(e, what);
@@ -2033,7 +2047,7 @@ int backward(const Call &c, const char *what) {
     if (c.rows == 0) {
         if (!c.accumulate) hipLaunchKernelGGL(k_clear, dim3(1024), dim3(256), 0, c.stream, c.dw, c.vocab * c.hidden);
     } else {
-        if (c.top && !l.few) launch_answers(c, l, true);
+        if (c.top && !l.few) launch_answers(c, l);
         for (int64_t first = 0; first < c.rows; first += l.rows) {
             const int64_t rows = std::min(l.rows, c.rows - first);
             const bool accumulate = c.accumulate || first > 0;

@@ -251,3 +251,27 @@ def test_a_token_with_a_channel_far_above_the_others(rows, outlier, dtype, top):
         if k in case:
             case[k][5] = 7
     _check_rows(f"outlier {outlier} in {rows} top {top} {dtype}", case, 2.0 if top else 1.0, but=5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,hidden,vocab,top,t", [(20, 1024, 5000, 64, 1.0), (24, 1021, 5000, 64, 1.0), (100, 2056, 700, 40, 1.0), (700, 1024, 5000, 64, 1.0), (1500, 4096, 2000, 64, 1.0),
+                                                     (900, 301, 2000, 200, 0.5)])
+def test_a_student_that_agrees_with_its_teacher(rows, hidden, vocab, top, t, dtype):
+    """The teacher's logits are the student's own largest: the loss is a small difference, whose logits have to come from the same sums to
+    cancel.  What cannot is the rounding of its terms, q log q and q log p, four of 2^-24."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    w = (torch.randn(vocab, hidden, generator=gen, device="cuda") / math.sqrt(hidden)).to(dtype)
+    x = (4 * torch.randn(rows, hidden, generator=gen, device="cuda")).to(dtype)
+    most = (x.double() @ w.double().t()).topk(top, 1)
+    case = dict(x=x, w=w, top_idx=most.indices.int(), top_logit=most.values.float(), row_grad=torch.full((rows,), 1 / rows, device="cuda"))
+    tag = f"agrees {rows}x{hidden}x{vocab} top {top} {dtype}"
+    print("head", tag, flush=True)
+    got, (want, terms) = _head_run(case, t), _exact(case, t)
+    log_q = torch.log_softmax(case["top_logit"].double() / t, 1)
+    log_p = most.values / t - want["lse"][:, None]
+    parts = t * t * (log_q.exp() * (log_q.abs() + log_p.abs())).sum(1)
+    off = (got["loss"].double() - want["loss"]).norm()
+    assert off <= 1e-5 * want["loss"].norm() + 2.0 ** -22 * parts.norm(), (tag, float(off / want["loss"].norm()), float(off / parts.norm()))
+    _close(f"{tag} lse", got["lse"], want["lse"].cpu(), F32)
+    for k, kind in (("dx", dtype), ("dw", F32)):
+        _close(f"{tag} {k}", got[k], want[k].cpu(), kind, terms[k].cpu())

@@ -67,34 +67,48 @@ class HeadSession(Session):
         binding.rsdgc_head_loss(self.y[:n], self.w, target, self.loss[:n], self.lse[:n], self.room)
         return self.loss[:n]
 
-    def step(self, x, target=None, top_idx=None, top_logit=None, share: float = 0.5, accumulate: bool = False):
-        """One microbatch: (loss of each row, dx), the parameters' gradients of the mean loss into the arena (accumulate: on top of
-        what is there).  With a target and a teacher's entries, `share` of the loss is the teacher's.  Both returned tensors are
-        overwritten by the next call."""
+    def step(self, x, target=None, top_idx=None, top_logit=None, share: float = 0.5, accumulate: bool = False, row_grad=None):
+        """One microbatch: (loss of each row, dx), the parameters' gradients into the arena (accumulate: on top of what is there).
+        They are those of the sum of the rows' losses times ``row_grad`` (float32, one for each row; None: 1 / rows, the mean over
+        all rows, in which one without a target counts as 0).  The mean over the rows that have a target:
+
+            has = (target >= 0).float()
+            head.step(x, target, row_grad=has / has.sum())
+
+        With a target and a teacher's entries, `share` of the loss is the teacher's.  Both returned tensors are overwritten by the
+        next call."""
         n = x.shape[0]
         taught = top_idx is not None
         assert 0 < n <= self.rows and (target is not None or taught) and (not taught or top_idx.shape[1] == self.top)
         part = share if taught and target is not None else 1.0 if taught else 0.0
         self._make_room(n)
-        y, dy, dx, loss, lse, row_grad = (t[:n] for t in (self.y, self.dy, self.dx, self.loss, self.lse, self.row_grad))
+        assert row_grad is None or (row_grad.shape == (n,) and row_grad.dtype == torch.float32)
+        y, dy, dx, loss, lse, gain = (t[:n] for t in (self.y, self.dy, self.dx, self.loss, self.lse, self.row_grad))
         mean, rstd, room = self.mean[:n], self.rstd[:n], self.room
         binding.rsdgc_layer_norm(x, self.gamma, self.beta, self.eps, y, mean, rstd)
         if target is not None:
             binding.rsdgc_head_loss(y, self.w, target, loss, lse, room)
-            row_grad.fill_((1.0 - part) / n)
-            binding.rsdgc_head_loss_backward(y, self.w, target, lse, row_grad, dy, self.dmatrix, accumulate, room)
+            self._gain(gain, row_grad, 1.0 - part)
+            binding.rsdgc_head_loss_backward(y, self.w, target, lse, gain, dy, self.dmatrix, accumulate, room)
         if taught:
             both = target is not None
             of_teacher, dy_taught = (self.loss_taught[:n], self.dy_taught[:n]) if both else (loss, dy)
             binding.rsdgc_distill_loss(y, self.w, top_idx, top_logit, self.temperature, of_teacher, lse, room)
-            row_grad.fill_(part / n)
-            binding.rsdgc_distill_loss_backward(y, self.w, top_idx, top_logit, self.temperature, lse, row_grad, dy_taught,
+            self._gain(gain, row_grad, part)
+            binding.rsdgc_distill_loss_backward(y, self.w, top_idx, top_logit, self.temperature, lse, gain, dy_taught,
                                                 self.dmatrix, accumulate or both, room)
             if both:
                 loss.mul_(1.0 - part).add_(of_teacher, alpha=part)
                 dy.add_(dy_taught)
         binding.rsdgc_layer_norm_backward(dy, x, self.gamma, mean, rstd, dx, self.dgamma, self.dbeta, accumulate, room)
         return loss, dx
+
+    @staticmethod
+    def _gain(out, row_grad, part: float) -> None:
+        if row_grad is None:
+            out.fill_(part / out.numel())
+        else:
+            torch.mul(row_grad, part, out=out)
 
     def apply(self, eta: float, messages: Optional[list] = None) -> None:
         """weights -= eta * (sum of the messages, in order; own one if none are given)."""

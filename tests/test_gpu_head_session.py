@@ -141,3 +141,30 @@ def test_what_the_binding_refuses():
             print("not refused:", n)
     with pytest.raises(TypeError):
         b.rsdgc_layer_norm(x.half(), None, None, 1e-5, x.half())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", [0, 5])
+def test_the_mean_over_the_rows_that_have_a_target(dtype, top):
+    """row_grad = 1 / count: the gradients of the mean over the rows with a target, however much padding there is."""
+    rows, hidden, vocab, share = 60, 64, 130, 0.25
+    gen = torch.Generator().manual_seed(7)
+    head = HeadSession(rows, hidden, vocab, dtype, ratio=0.2, top=top, temperature=2.0)
+    head.set_weights(1 + 0.1 * torch.randn(hidden, generator=gen), 0.1 * torch.randn(hidden, generator=gen),
+                     torch.randn(vocab, hidden, generator=gen) / math.sqrt(hidden))
+    x = torch.randn(rows, hidden, generator=gen).to(dtype).cuda()
+    target = torch.randint(0, vocab, (rows,), generator=gen).int().cuda()
+    target[20:] = -1
+    taught = {}
+    if top:
+        idx = torch.stack([torch.randperm(vocab, generator=gen)[:top] for _ in range(rows)]).int().cuda()
+        taught = dict(top_idx=idx, top_logit=(3 * torch.randn(rows, top, generator=gen)).cuda(), share=share)
+    has = (target >= 0).float()
+    # the rows that have a target alone: their mean over 20 is the reference's mean over its rows
+    kept = {k: v[:20] if k != "share" else v for k, v in taught.items()}
+    args = (head, x[:20], target[:20], kept.get("top_idx"), kept.get("top_logit"), share)
+    want, moved = (_exact(*args, ulps) for ulps in (0.0, 1.0))
+    _, dx = head.step(x, target, row_grad=has / has.sum(), **taught)
+    for tag, got, value, other in zip(("dx", "dgamma", "dbeta", "dmatrix"), (dx[:20], head.dgamma, head.dbeta, head.dmatrix), want[1:], moved[1:]):
+        _near(tag, got, value, REL[dtype], other)
+    assert float(dx[20:].float().abs().max()) == 0.0

@@ -420,8 +420,9 @@ int rsdgc_last_paths_blocks(rsdgc_plan_t *plan, const void *workspace, int32_t *
  * No plan is needed.  Calls enqueue kernels only, may be captured, and allocate nothing;
  * `workspace` [device] holds nothing between calls and may be shared by calls that follow
  * each other on one stream.  What a call writes must not overlap what it reads or writes
- * otherwise (RSDGC_EINVAL), except where a form in place is named.  Sums are formed in a
- * fixed order: the same inputs give the same bits.                                   */
+ * otherwise (RSDGC_EINVAL), except where a form in place is named; columns of one buffer side by
+ * side, with the same stride, do not overlap.  Sums are formed in a fixed order: the same inputs
+ * give the same bits.                                                                */
 #define RSDGC_F32   0
 #define RSDGC_BF16  1
 

@@ -1977,15 +1977,13 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
 bool sizes_ok(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab) {
     return type_known(dtype) && rows >= 0 && rows <= kMaxRows && hidden >= 1 && hidden <= kMaxStride && vocab >= 1 && vocab <= kMaxVocab;
 }
-struct Range { const void *p; size_t n; };
-
 // What a call writes may touch nothing else that it reads or writes.
 bool apart(const Range *written, int n_written, const Range *read, int n_read) {
     for (int i = 0; i < n_written; ++i) {
         for (int j = i + 1; j < n_written; ++j)
-            if (ranges_overlap(written[i].p, written[i].n, written[j].p, written[j].n)) return false;
+            if (ranges_overlap(written[i], written[j])) return false;
         for (int j = 0; j < n_read; ++j)
-            if (ranges_overlap(written[i].p, written[i].n, read[j].p, read[j].n)) return false;
+            if (ranges_overlap(written[i], read[j])) return false;
     }
     return true;
 }
@@ -2000,8 +1998,8 @@ bool inputs_ok(const Call &c) {
 }
 void read_by(const Call &c, Range (&r)[4]) {
     const size_t size = type_size(c.dtype), entries = static_cast<size_t>(c.rows) * std::max(1, c.top) * 4;
-    r[0] = {c.x, extent_bytes(c.rows, c.hidden, c.ldx, size)};
-    r[1] = {c.w, extent_bytes(c.vocab, c.hidden, c.ldw, size)};
+    r[0] = matrix_range(c.x, c.rows, c.hidden, c.ldx, size);
+    r[1] = matrix_range(c.w, c.vocab, c.hidden, c.ldw, size);
     r[2] = {c.idx, entries};
     r[3] = {c.logit, c.top ? entries : 0};
 }
@@ -2042,7 +2040,7 @@ int backward(const Call &c, const char *what) {
     read_by(c, four);
     read[4] = {c.lse, static_cast<size_t>(c.rows) * 4};
     read[5] = {c.row_grad, static_cast<size_t>(c.rows) * 4};
-    const Range written[] = {{c.dx, extent_bytes(c.rows, c.hidden, c.lddx, size)}, {c.dw, static_cast<size_t>(c.vocab) * c.hidden * 4}, {c.ws, l.total}};
+    const Range written[] = {matrix_range(c.dx, c.rows, c.hidden, c.lddx, size), {c.dw, static_cast<size_t>(c.vocab) * c.hidden * 4}, {c.ws, l.total}};
     if (!apart(written, 3, read, 6)) return RSDGC_EINVAL;
     if (c.rows == 0) {
         if (!c.accumulate) hipLaunchKernelGGL(k_clear, dim3(1024), dim3(256), 0, c.stream, c.dw, c.vocab * c.hidden);

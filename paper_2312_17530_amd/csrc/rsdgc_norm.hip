@@ -414,7 +414,7 @@ bool sizes_ok(int32_t dtype, int64_t rows, int64_t cols) { return type_known(dty
 // a and b may be the same rows, or apart; not shifted against each other.
 bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t cols, size_t size) {
     if (a == b && lda == ldb) return true;
-    return !ranges_overlap(a, extent_bytes(rows, cols, lda, size), b, extent_bytes(rows, cols, ldb, size));
+    return !ranges_overlap(matrix_range(a, rows, cols, lda, size), matrix_range(b, rows, cols, ldb, size));
 }
 
 }  // namespace

@@ -26,6 +26,23 @@ inline bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb) {
     return a && b && na && nb && x < y + nb && y < x + na;
 }
 
+// What an operand takes in memory; of a matrix also the bytes from row to row and of a row.
+struct Range {
+    const void *p;
+    size_t n, pitch, row;
+};
+inline Range matrix_range(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size) {
+    return {p, extent_bytes(rows, cols, ld, size), static_cast<size_t>(ld) * size, static_cast<size_t>(cols) * size};
+}
+// Columns of one buffer side by side do not overlap, though one begins before the other ends.
+inline bool ranges_overlap(const Range &a, const Range &b) {
+    if (!ranges_overlap(a.p, a.n, b.p, b.n)) return false;
+    if (!a.pitch || a.pitch != b.pitch) return true;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    const size_t off = y >= x ? (y - x) % a.pitch : (a.pitch - (x - y) % a.pitch) % a.pitch;       // of b's rows behind a's
+    return off < a.row || off + b.row > a.pitch;
+}
+
 typedef __bf16 bf16;
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return static_cast<float>(v); }

@@ -131,3 +131,22 @@ def test_the_widest_rows_return():
 @pytest.mark.parametrize("t", [2e-39, 1e-45])
 def test_a_temperature_without_a_reciprocal_is_refused(name, base, t):
     assert _call(name, base, dict(t=t)) == b.RSDGC_EINVAL
+
+
+# Two matrices side by side in one buffer: 64 columns each, rows 128 elements apart
+SIDE = [("rsdgc_layer_norm", NORM, "ldx", "x", "ldy", "y"), ("rsdgc_layer_norm_backward", NORM_BACK, "ldx", "x", "lddx", "dx"),
+        ("rsdgc_layer_norm_backward", NORM_BACK, "lddy", "dy", "lddx", "dx"), ("rsdgc_head_loss_backward", HEAD_BACK, "ldx", "x", "lddx", "dx"),
+        ("rsdgc_distill_loss_backward", TAUGHT_BACK, "ldx", "x", "lddx", "dx")]
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="the addresses are numbers: only where no kernel can be launched")
+@pytest.mark.parametrize("name,base,ld_a,a,ld_b,b_", SIDE, ids=[f"{n}-{a}" for n, _, _, a, _, _ in SIDE])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_columns_of_one_buffer_side_by_side_are_taken(name, base, ld_a, a, ld_b, b_, dtype):
+    size = 2 if dtype else 4
+    for at in (64 * size, -64 * size, (128 - 64) * size):
+        assert _call(name, base, {"dtype": dtype, ld_a: 128, ld_b: 128, a: X + 4096, b_: X + 4096 + at}) == b.RSDGC_EHIP, at
+    # one element into each other, from either side, or rows of another length
+    for at in (63 * size, -63 * size, 65 * size, -65 * size):
+        assert _call(name, base, {"dtype": dtype, ld_a: 128, ld_b: 128, a: X + 4096, b_: X + 4096 + at}) == b.RSDGC_EINVAL, at
+    assert _call(name, base, {"dtype": dtype, ld_a: 128, ld_b: 136, a: X + 4096, b_: X + 4096 + 64 * size}) == b.RSDGC_EINVAL

@@ -445,9 +445,9 @@ def _stream_on(t, stream) -> Optional[int]:
     return _stream(stream)
 
 
-def _rows(t, dtype, shape, where: str):
-    """(address, stride between rows) of a matrix of `shape` whose rows are without gaps."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+def _rows(t, dtype, shape, dev: int, where: str):
+    """(address, stride between rows) of a matrix of `shape` on device `dev` whose rows are without gaps."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         _need(False, where)
     rows, cols = shape
     down, along = t.stride()
@@ -457,39 +457,39 @@ def _rows(t, dtype, shape, where: str):
     return t.data_ptr(), (down if rows > 1 else cols)
 
 
-def _flat(t, n: int, dtype, where: str) -> Optional[int]:
-    """Address of n elements without gaps."""
+def _flat(t, n: int, dtype, dev: int, where: str) -> Optional[int]:
+    """Address of n elements on device `dev` without gaps."""
     if t is None:
         return None
-    if t.numel() != n or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if t.numel() != n or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
         _need(False, where)
     return t.data_ptr()
 
 
-def _bytes(workspace, need: int, where: str) -> Optional[int]:
-    _need(workspace is not None and workspace.is_contiguous() and workspace.is_cuda
+def _bytes(workspace, need: int, dev: int, where: str) -> Optional[int]:
+    _need(workspace is not None and workspace.is_contiguous() and workspace.get_device() == dev
           and workspace.numel() * workspace.element_size() >= need, where)
     return workspace.data_ptr()
 
 
 def _matrix(x, where: str):
-    """(library, code, shape) of the operand that the others follow."""
+    """(library, code, shape, device) of the operand that the others follow; no kernel can read another device's memory."""
     lib = _training()
-    shape = x.shape
-    _need(len(shape) == 2, where)
-    return lib, _dtype(x.dtype), shape
+    shape, dev = x.shape, x.get_device()
+    _need(len(shape) == 2 and dev >= 0, where)
+    return lib, _dtype(x.dtype), shape, dev
 
 
 def rsdgc_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
     """y = (x - mean) * rstd * gamma + beta over the rows of x; mean and rstd are kept for the backward pass if given."""
     where = "rsdgc_layer_norm"
-    lib, code, shape = _matrix(x, where)
+    lib, code, shape, dev = _matrix(x, where)
     rows, cols = shape
-    px, ldx = _rows(x, x.dtype, shape, where)
-    py, ldy = _rows(y, x.dtype, shape, where)
+    px, ldx = _rows(x, x.dtype, shape, dev, where)
+    py, ldy = _rows(y, x.dtype, shape, dev, where)
     f32 = _torch.float32
-    _check(lib.rsdgc_layer_norm(code, rows, cols, px, ldx, _flat(gamma, cols, f32, where), _flat(beta, cols, f32, where), eps,
-                                py, ldy, _flat(mean, rows, f32, where), _flat(rstd, rows, f32, where), _stream_on(x, stream)),
+    _check(lib.rsdgc_layer_norm(code, rows, cols, px, ldx, _flat(gamma, cols, f32, dev, where), _flat(beta, cols, f32, dev, where), eps,
+                                py, ldy, _flat(mean, rows, f32, dev, where), _flat(rstd, rows, f32, dev, where), _stream_on(x, stream)),
            where)
 
 
@@ -502,19 +502,19 @@ def rsdgc_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
 def rsdgc_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, accumulate: bool, workspace, stream=None) -> None:
     """dx, and dgamma / dbeta (float32, e.g. layers of the gradient arena; None: not wanted) of rsdgc_layer_norm."""
     where = "rsdgc_layer_norm_backward"
-    lib, code, shape = _matrix(x, where)
+    lib, code, shape, dev = _matrix(x, where)
     rows, cols = shape
-    px, ldx = _rows(x, x.dtype, shape, where)
-    pdy, lddy = _rows(dy, x.dtype, shape, where)
-    pdx, lddx = _rows(dx, x.dtype, shape, where)
+    px, ldx = _rows(x, x.dtype, shape, dev, where)
+    pdy, lddy = _rows(dy, x.dtype, shape, dev, where)
+    pdx, lddx = _rows(dx, x.dtype, shape, dev, where)
     _need(mean is not None and rstd is not None, where)
     ws = None
     if dgamma is not None or dbeta is not None:
-        ws = _bytes(workspace, lib.rsdgc_layer_norm_workspace_bytes(rows, cols), where)
+        ws = _bytes(workspace, lib.rsdgc_layer_norm_workspace_bytes(rows, cols), dev, where)
     f32 = _torch.float32
-    _check(lib.rsdgc_layer_norm_backward(code, rows, cols, pdy, lddy, px, ldx, _flat(gamma, cols, f32, where),
-                                         _flat(mean, rows, f32, where), _flat(rstd, rows, f32, where), pdx, lddx,
-                                         _flat(dgamma, cols, f32, where), _flat(dbeta, cols, f32, where),
+    _check(lib.rsdgc_layer_norm_backward(code, rows, cols, pdy, lddy, px, ldx, _flat(gamma, cols, f32, dev, where),
+                                         _flat(mean, rows, f32, dev, where), _flat(rstd, rows, f32, dev, where), pdx, lddx,
+                                         _flat(dgamma, cols, f32, dev, where), _flat(dbeta, cols, f32, dev, where),
                                          1 if accumulate else 0, ws, _stream_on(x, stream)), where)
 
 
@@ -527,23 +527,23 @@ def rsdgc_head_workspace_bytes(dtype, rows: int, hidden: int, vocab: int, top: i
 
 def _head(x, w, top: int, workspace, backward: bool, where: str):
     """The library, the arguments that the head's calls begin with, and the workspace's address."""
-    lib, code, shape = _matrix(x, where)
+    lib, code, shape, dev = _matrix(x, where)
     rows, hidden = shape
     _need(w.dim() == 2 and w.shape[1] == hidden, where)
-    px, ldx = _rows(x, x.dtype, shape, where)
-    pw, ldw = _rows(w, x.dtype, w.shape, where)
+    px, ldx = _rows(x, x.dtype, shape, dev, where)
+    pw, ldw = _rows(w, x.dtype, w.shape, dev, where)
     vocab = w.shape[0]
     need = lib.rsdgc_head_workspace_bytes(code, rows, hidden, vocab, top, 1 if backward else 0)
     _need(need > 0, where)
-    return lib, (code, rows, hidden, vocab, px, ldx, pw, ldw), _bytes(workspace, need, where)
+    return lib, (code, rows, hidden, vocab, px, ldx, pw, ldw), _bytes(workspace, need, dev, where)
 
 
 def _head_gradients(x, w, lse, row_grad, dx, dw, accumulate: bool, where: str):
-    rows, hidden = x.shape
+    (rows, hidden), dev = x.shape, x.get_device()
     f32 = _torch.float32
-    pdx, lddx = _rows(dx, x.dtype, x.shape, where)
+    pdx, lddx = _rows(dx, x.dtype, x.shape, dev, where)
     _need(lse is not None and row_grad is not None and dw is not None, where)
-    return (_flat(lse, rows, f32, where), _flat(row_grad, rows, f32, where), pdx, lddx, _flat(dw, w.shape[0] * hidden, f32, where),
+    return (_flat(lse, rows, f32, dev, where), _flat(row_grad, rows, f32, dev, where), pdx, lddx, _flat(dw, w.shape[0] * hidden, f32, dev, where),
             1 if accumulate else 0)
 
 
@@ -551,8 +551,8 @@ def rsdgc_head_loss(x, w, target, loss, lse, workspace, stream=None) -> None:
     """Softmax cross entropy of the logits x w^T against target (int32; outside the vocabulary: no answer), per row."""
     where = "rsdgc_head_loss"
     lib, args, ws = _head(x, w, 0, workspace, False, where)
-    n, f32 = x.shape[0], _torch.float32
-    _check(lib.rsdgc_head_loss(*args, _flat(target, n, _torch.int32, where), _flat(loss, n, f32, where), _flat(lse, n, f32, where),
+    n, f32, dev = x.shape[0], _torch.float32, x.get_device()
+    _check(lib.rsdgc_head_loss(*args, _flat(target, n, _torch.int32, dev, where), _flat(loss, n, f32, dev, where), _flat(lse, n, f32, dev, where),
                                ws, _stream_on(x, stream)), where)
 
 
@@ -560,7 +560,7 @@ def rsdgc_head_loss_backward(x, w, target, lse, row_grad, dx, dw, accumulate: bo
     """dx, and dw (float32, vocabulary x width without gaps, e.g. a layer of the gradient arena), of rsdgc_head_loss."""
     where = "rsdgc_head_loss_backward"
     lib, args, ws = _head(x, w, 0, workspace, True, where)
-    _check(lib.rsdgc_head_loss_backward(*args, _flat(target, x.shape[0], _torch.int32, where),
+    _check(lib.rsdgc_head_loss_backward(*args, _flat(target, x.shape[0], _torch.int32, x.get_device(), where),
                                         *_head_gradients(x, w, lse, row_grad, dx, dw, accumulate, where), ws,
                                         _stream_on(x, stream)), where)
 
@@ -569,8 +569,8 @@ def _teacher(x, top_idx, top_logit, where: str):
     _training()
     _need(top_idx.dim() == 2 and top_idx.shape[0] == x.shape[0] and top_logit.shape == top_idx.shape
           and 1 <= top_idx.shape[1] <= RSDGC_MAX_TOP, where)
-    n = top_idx.numel()
-    return top_idx.shape[1], _flat(top_idx, n, _torch.int32, where), _flat(top_logit, n, _torch.float32, where)
+    n, dev = top_idx.numel(), x.get_device()
+    return top_idx.shape[1], _flat(top_idx, n, _torch.int32, dev, where), _flat(top_logit, n, _torch.float32, dev, where)
 
 
 def rsdgc_distill_loss(x, w, top_idx, top_logit, temperature: float, loss, lse, workspace, stream=None) -> None:
@@ -578,8 +578,8 @@ def rsdgc_distill_loss(x, w, top_idx, top_logit, temperature: float, loss, lse, 
     where = "rsdgc_distill_loss"
     top = _teacher(x, top_idx, top_logit, where)
     lib, args, ws = _head(x, w, top[0], workspace, False, where)
-    n, f32 = x.shape[0], _torch.float32
-    _check(lib.rsdgc_distill_loss(*args, *top, temperature, _flat(loss, n, f32, where), _flat(lse, n, f32, where), ws,
+    n, f32, dev = x.shape[0], _torch.float32, x.get_device()
+    _check(lib.rsdgc_distill_loss(*args, *top, temperature, _flat(loss, n, f32, dev, where), _flat(lse, n, f32, dev, where), ws,
                                   _stream_on(x, stream)), where)
 
 

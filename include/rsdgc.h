@@ -468,7 +468,8 @@ int rsdgc_head_loss(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, 
  *   dx        [device] rows x hidden of dtype,  dw [device] float32, vocab x hidden without gaps.
  * Each element of d counts with 22 bits (in dx of few bfloat16 rows with 16) down to 2^-40 of the
  * row's largest, whatever the other rows' row_grad is; in dw of many rows row_grad * x counts with
- * 22 bits (bfloat16: as it is) down to 2^-40 of the largest of the call's rows.
+ * 22 bits (bfloat16: as it is) down to 2^-40 of the largest of the call's rows, and in dx of many
+ * bfloat16 rows W down to 2^-40 of its piece's largest.
  * rows = 0 zeroes dw, or leaves it with accumulate.                                  */
 int rsdgc_head_loss_backward(int32_t dtype, int64_t rows, int64_t hidden, int64_t vocab, const void *x, int64_t ldx,
                              const void *w, int64_t ldw, const int32_t *target, const float *lse, const float *row_grad,

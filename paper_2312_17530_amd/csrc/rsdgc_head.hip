@@ -28,11 +28,11 @@
 //              the reading of W, and W is not gone over beforehand: float32 W is split on its way from memory to registers.
 //
 // What it measured (all of a forward and backward pass; W's rows by width by tokens):
-//   131072 x 4096 x 8192 bfloat16   stats 7.1 ms = 1.24 PFLOP/s, d 7.3 (1.20), dx 7.8 (1.13), dW 12.2 to 12.5 of two products (1.42); a
-//                                   large library product on this card reaches 1.44.  Bound by the matrix instructions' rate under
-//                                   the card's power (busy 62 to 83 % of the cycles); d loses to its epilogue, 4 bytes of planes for
-//                                   each logit
-//   32000 x 1024 x 2048 float32     376 + 397 + 342 + 345 us, three products each: 1.1 PFLOP/s of 16-bit products, 370 TFLOP/s of
+//   131072 x 4096 x 8192 bfloat16   stats 6.7 to 7.1 ms = 1.24 to 1.32 PFLOP/s, d 7.2 (1.23), dx 13.9 of two products (1.27), dW 12.5 of
+//                                   two products (1.40); a large library product on this card reaches 1.44.  Bound by the matrix
+//                                   instructions' rate under the card's power (busy 60 to 84 % of the cycles); d loses to its epilogue,
+//                                   4 bytes of planes for each logit
+//   32000 x 1024 x 2048 float32     383 + 406 + 350 + 356 us, three products each: 1.1 PFLOP/s of 16-bit products, 360 TFLOP/s of
 //                                   float32 ones, where the float32 matrix instructions reach 150
 //   65536 x 4096 x 1 bfloat16       104 us for 537 MB: 5.2 TB/s, bound by memory
 #include "rsdgc_gemm.h"
@@ -65,10 +65,10 @@ constexpr float kNoExponent = -10000.0f;           // of nothing
 
 // Up to so many rows a call takes the form for few rows.  Measured, few / many, us, W of 32768 rows (as is: both read as they lie):
 //   loss alone                     with gradients
-//   float32   x 4096  384 rows: 574 / 707, 512: 710 / 735, 768: 1025 / 888     128 rows: 960 / 1405, 192: 1518 / 1587, 256: 1767 / 1733
-//   float32   x 515   384 rows: 88 / 88, 512: 119 / 97                         128 rows: 203 / 222, 192: 249 / 230
-//   bfloat16  x 4097  384 rows: 189 / 321, 1024: 433 / 440, 2048: 829 / 685    192 rows: 951 / 1275, 256: 1221 / 1365, 333: 1571 / 1409
-//   bfloat16  x 4096, as is: the same                                          128 rows: 543 / 617, 192: 810 / 690
+//   float32   x 4096  384 rows: 556 / 710, 512: 704 / 732, 768: 1036 / 876     128 rows: 957 / 1465, 192: 1533 / 1605, 256: 1760 / 1664
+//   float32   x 515   384 rows: 84 / 90, 512: 110 / 96                         128 rows: 198 / 200, 192: 250 / 242
+//   bfloat16  x 4097  384 rows: 187 / 323, 1024: 430 / 445, 2048: 829 / 684    192 rows: 951 / 1298, 256: 1220 / 1365, 333: 1566 / 1504
+//   bfloat16  x 4096, as is: the same                                          128 rows: 539 / 633, 160: 757 / 703, 192: 809 / 727
 int64_t few_rows(int32_t dtype, bool as_is, bool backward) {
     const bool unaligned = dtype == RSDGC_BF16 && !as_is;
     return backward ? (unaligned ? 256 : 160) : unaligned ? 1024 : 384;
@@ -180,7 +180,7 @@ __device__ __forceinline__ void load_chunk(const T *row, int c, int cols, float 
 }
 
 // The exponent of the largest finite magnitude of a matrix; a partial result per workgroup.  Bound by memory: 16384 x 4096 bfloat16, a piece of W,
-// 38.7 us = 3.5 TB/s (16 bytes a thread, no atomics: a search's order must not matter).
+// 41 us = 3.3 TB/s (16 bytes a thread, no atomics: a search's order must not matter).
 template <typename T>
 __global__ __launch_bounds__(256) void k_largest(const T *x, int64_t rows, int32_t cols, int64_t ld, float *parts) {
     __shared__ float red[4];
@@ -228,7 +228,7 @@ __device__ __forceinline__ uint16_t bits(bf16 v) { return __builtin_bit_cast(uin
 
 // A matrix as float16 planes under the scale that `parts` gives (hi, and lo where it is wanted), rows of `ld_out` (a multiple
 // of 8) elements, zeros beyond cols.  gain not NULL: each row times the power of two of its gain, zeros where the gain is 0.
-// Bound by memory: 16384 x 4096 bfloat16 to one plane 42 us = 6.4 TB/s, its reads still in the cache from the search before.
+// Bound by memory: 16384 x 4096 bfloat16 to one plane 43 us = 6.3 TB/s, its reads still in the cache from the search before.
 template <typename T>
 __global__ __launch_bounds__(256) void k_planes(const T *x, int64_t rows, int32_t cols, int64_t ld, const float *gain, const float *parts, int32_t n_parts,
                                                 int32_t *shift_out, uint16_t *hi, uint16_t *lo, int32_t ld_out) {
@@ -533,7 +533,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_stats(const Problem p, const
 }
 
 // lse from a token's strips, and the loss, a wave for each token.  picked: the logits of its one target (see Picked), or of a teacher's
-// entries, whose shares are formed here.
+// entries, whose shares are formed here.  4096 tokens: 7 us for a target, 13 behind 64 entries.  To hand 64 entries a token on costs k_stats
+// 12 % (65536 x 2048 x 4096 bfloat16 979 / 1097 us), dot products with W's rows here cost 164 us.
 template <bool TAUGHT>
 __global__ __launch_bounds__(256) void k_loss(int64_t rows, const float2 *stats, int32_t strips, const int32_t *target, const float *picked, int32_t vocab, const Teacher teacher, float t,
                                               float *loss, float *lse_out) {
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(256) void k_loss(int64_t rows, const float2 *stats,
 
 // ----------------------------------------------------------------- backward
 // C[n][v]: d as planes.  PAIRED: two neighbouring columns a lane, so that a store takes 4 bytes.  A piece of
-// d takes kPieceBytes at most (two passes of 131072 x 4096 x 8192: 38.9 ms with 128 MB, 35.9 with 256, 35.2 with 512).
+// d takes kPieceBytes at most (two passes of 131072 x 4096 x 8192: 43.3 ms with 128 MB, 41.0 with 256, 40.6 with 512).
 struct GradArgs {
     int many;                          // many rows: d has the gain's fraction alone (gain_in_d)
     const int32_t *shift_x, *shift_w;  // of scaled planes that the logits come from, by row and of the piece; NULL: none
@@ -1265,7 +1266,7 @@ template <> struct Four<bf16> {
 // NARROW: fewer than four columns in all, loaded one by one.
 template <typename T, int NB, bool NARROW>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 1 : 2) void k_few_input(const FewInput<T> a) {
-    constexpr int P = kPlanesOf<T>, D = P == 3 ? 3 : 2;              // bfloat16, the result's type: 16 bits of d are enough
+    constexpr int P = kPlanesOf<T>, D = P == 3 ? 3 : 2;              // bfloat16, the result's type: two planes of d are good to 2^-18, a float32 sum's error
     __shared__ float tile[2][32 * NB][128 + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     int at, group, part;
@@ -1504,8 +1505,8 @@ struct Choice {
     Tile tile;
     int64_t splits;
 };
-// Both passes, us, with the largest tile 256 / 128 / 64: bfloat16 10007 x 1000 under 777 rows 172 / 191 / 243 (the rule 166),
-// 50021 x 2048 under 4096 3947 / 4725 / 8726; a unit of 2.5 instead of 3 for 64: float32 4096 x 2048 under 1024 rows 343 for 294.
+// Both passes, us, with the largest tile 256 / 128 / 64: bfloat16 10007 x 1000 under 777 rows 181 / 204 / 256, 50021 x 2048
+// under 4096 4317 / 5504 / 9312; a unit of 2.5 instead of 3 for 64: float32 4096 x 2048 under 1024 rows 349 for 301.
 // A round over all CUs takes so many units of time per stage of 64 k (measured: the larger tiles move fewer bytes per product,
 // the small ones leave fewer CUs without work).  The k axis is cut into shares where the tiles alone do not fill the CUs.
 Choice choose(int64_t m, int64_t n, int64_t k, int64_t splits_most, Tile largest = kTile256) {
@@ -1949,7 +1950,7 @@ void launch_backward(const Call &c, const Layout &l, int64_t first_row, int64_t 
             Problem p = problem(d_planes, wd, rows, c.hidden, count);
             Choice how = choose(rows, c.hidden, count, l.splits_most);
             if (wide_dx(c.dtype, c.rows, c.hidden)) how = {kTileWide, std::max<int64_t>(1, std::min<int64_t>(l.splits_most, 512 / ((c.hidden + 255) / 256)))};
-            constexpr int kForDx = D_PLANES == 3 ? 2 : D_PLANES;      // bfloat16: the third plane is below what dx can hold
+            constexpr int kForDx = D_PLANES == 3 ? 2 : D_PLANES;      // bfloat16, few rows: two planes of d are good to 2^-18, a float32 sum's error
             with_shape<D, false, true, false, kForDx, PLANES>(how.tile, [&](auto shape) {
                 using S = decltype(shape);
                 const dim3 grid = cut<S>(p, how.splits);

@@ -9,8 +9,8 @@
 // thread that owns the columns while its group goes from row to row; each workgroup then leaves one line of partial sums and
 // a second launch adds the lines up in a fixed order.  Everything is summed in float32.
 //
-// Bound by memory.  Forward 65536 x 2048 bfloat16 96 us = 5.6 TB/s (read and written), backward 176 us = 4.6 TB/s and 6 us for the lines;
-// 8192 x 4096 24 and 52 + 5 us; one row of 4096 3 us, a launch.  A copy of this size reaches 5.1 TB/s on this card.
+// Bound by memory.  Forward 65536 x 2048 bfloat16 97 us = 5.5 TB/s (read and written), backward 174 us = 4.6 TB/s and 6 us for the lines;
+// 8192 x 4096 25 and 51 + 5 us; one row of 4096 3 us, a launch.  A copy of this size reaches 5.1 TB/s on this card.
 #include "rsdgc_training.h"
 
 #include <algorithm>
